@@ -159,6 +159,45 @@ prism_status prism_route(const prism_layer_desc* desc, const void* x, const void
                          float* topk_gate, int32_t* counts, int64_t* counts_accum, void* stream);
 
 /*
+ * Training a router: the balance loss of a batch's routing with its activation counts, and the gradient of
+ * that loss and of the gates with respect to the router logits.
+ *
+ * Tokens come in groups (sequences): token t belongs to group t / group_tokens, the last one may be shorter;
+ * group_tokens == 0 makes one group of all.  G = 1 if group_tokens is 0, else ceil(T / group_tokens), at most
+ * PRISM_MAX_BALANCE_GROUPS (beyond: UNSUPPORTED).  A token counts if token_mask is NULL or token_mask[t] != 0;
+ * what the others' logits, picks and gate gradients hold (padding) is never used.
+ *   logits      [T,E] fp32, as prism_route returns them: finite, or -inf for an expert that cannot be picked
+ *   topk_idx    [T,k] int32; a pick outside [0, E) is none
+ *   n_tokens[g] = tokens of group g that count                                    [G] int32
+ *   counts[g,e] = their picks of expert e                                         [G,E] int32
+ *   probs[g,e]  = mean over them of softmax(logits[t])[e]                         [G,E] fp32
+ *   loss[g]     = E / (k n_tokens[g]) * sum_e counts[g,e] probs[g,e]              [G] fp32
+ *                 (1 for an even spread; all of these are 0 for a group without tokens)
+ * Sums over tokens run in an order that depends on the sizes alone.  The workspace (256-byte aligned, at least
+ * prism_balance_workspace_bytes, which depends on E alone) holds partial sums during the call.
+ */
+#define PRISM_MAX_BALANCE_GROUPS (1 << 23)
+prism_status prism_balance_workspace_bytes(const prism_layer_desc* desc, size_t* bytes);
+prism_status prism_balance_loss(const prism_layer_desc* desc, const float* logits, const int32_t* topk_idx,
+                                const uint8_t* token_mask, int32_t group_tokens, int32_t T, float* loss,
+                                int32_t* counts, float* probs, int32_t* n_tokens, void* workspace,
+                                size_t workspace_bytes, void* stream);
+
+/*
+ * The backward pass of prism_route's gates and of prism_balance_loss:
+ *   d_logits[t,e] = sum_g d_loss[g] * d loss[g] / d logits[t,e]  +  sum_j d_gate[t,j] * d topk_gate[t,j] / d logits[t,e]
+ * The counts and the picks are constants (they are steps of the logits).  The gates are those of desc->gate_mode, over
+ * the picks in [0, E); an expert picked twice by a token collects both.
+ *   d_loss  [G] fp32 with counts [G,E] and n_tokens [G] of prism_balance_loss for the same T and group_tokens, or all
+ *           three NULL for no such term;  d_gate [T,k] fp32 or NULL for none (then topk_idx may be NULL); not both NULL
+ *   d_logits  [T,E] fp32 out, overwritten; zeros for a token that does not count
+ */
+prism_status prism_route_backward(const prism_layer_desc* desc, const float* logits, const int32_t* topk_idx,
+                                  const uint8_t* token_mask, int32_t group_tokens, int32_t T, const int32_t* counts,
+                                  const int32_t* n_tokens, const float* d_loss, const float* d_gate, float* d_logits,
+                                  void* stream);
+
+/*
  * Placement split (Sec. III-B, indicator 1_remote) and stable bucketing.
  * Assignment a = t*k + j is local iff local_mask[topk_idx[a]] != 0.
  *   local_src      [T*k] int32 out: the local assignments, bucketed by expert

@@ -22,7 +22,7 @@ SYMBOLS = ("prism_status_string", "prism_workspace_bytes", "prism_route", "prism
            "prism_ceiling_mfma_bf16", "prism_ceiling_hbm_read", "prism_pack_remote",
            "prism_combine_remote", "prism_debug_check_weights", "prism_pack_weights",
            "prism_layer_permutation", "prism_moe_layer_static", "prism_ceiling_hbm_read_pattern",
-           "prism_clear_rows")
+           "prism_clear_rows", "prism_balance_workspace_bytes", "prism_balance_loss", "prism_route_backward")
 STAGES = ("route", "dispatch", "ffn_up", "ffn_down", "combine")
 GATE_MODES = {"renormalized": 0, "softmax_all": 1}
 WEIGHT_LAYOUTS = {"row_major": 0, "tiled": 1}
@@ -66,6 +66,9 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.prism_status_string.argtypes = [ctypes.c_int]
     lib.prism_workspace_bytes.argtypes = [dp, i32, ctypes.POINTER(sz)]
     lib.prism_route.argtypes = [dp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp]
+    lib.prism_balance_workspace_bytes.argtypes = [dp, ctypes.POINTER(sz)]
+    lib.prism_balance_loss.argtypes = [dp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, sz, vp]
+    lib.prism_route_backward.argtypes = [dp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp]
     lib.prism_dispatch.argtypes = [dp, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.prism_expert_ffn.argtypes = [dp, vp, wp, vp, vp, i32, vp, vp, sz, vp]
     lib.prism_combine.argtypes = [dp, vp, vp, vp, vp, i32, vp, vp, sz, vp]
@@ -177,6 +180,82 @@ def prism_route(desc: LayerDesc, x, w_router, router_bias, want_logits=True, cou
     return RouteOut(logits, idx, gate, counts)
 
 
+def alloc_balance_workspace(desc: LayerDesc, device="cuda") -> torch.Tensor:
+    n = ctypes.c_size_t(0)
+    _check(load_library().prism_balance_workspace_bytes(ctypes.byref(desc), ctypes.byref(n)),
+           "prism_balance_workspace_bytes")
+    return torch.empty(n.value, dtype=torch.uint8, device=device)
+
+
+def _typed(t: Optional[torch.Tensor], dtype: torch.dtype, shape, what: str) -> Optional[int]:
+    """The address of a tensor that has to be of this type and shape, on the device the call is enqueued on."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise PrismError(f"{what} has to be {dtype} {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
+    if t.device.index != torch.cuda.current_device():
+        raise PrismError(f"{what} is on {t.device}, not on the current device")
+    return _ptr(t)
+
+
+@dataclass
+class BalanceOut:
+    loss: torch.Tensor          # [G]
+    counts: torch.Tensor        # [G, E]
+    probs: torch.Tensor         # [G, E]
+    n_tokens: torch.Tensor      # [G]
+
+
+def _balance_groups(T: int, group_tokens: int) -> int:
+    return -(-T // group_tokens) if group_tokens > 0 else 1
+
+
+def prism_balance_loss(desc: LayerDesc, logits, topk_idx, workspace, token_mask=None, group_tokens: int = 0,
+                       outputs: Optional[BalanceOut] = None, stream=None) -> BalanceOut:
+    """Balance loss, activation counts and mean probabilities of every group of tokens (see prism.h).
+
+    logits [T, E] and topk_idx [T, k] as prism_route returns them; token_mask [T] uint8, 0 for padding."""
+    T, E, k = logits.shape[0], desc.n_experts, desc.top_k
+    G, dev = _balance_groups(T, group_tokens), logits.device
+    f32, i32 = torch.float32, torch.int32
+    o = outputs
+    if o is None:
+        o = BalanceOut(torch.empty((G,), dtype=f32, device=dev), torch.empty((G, E), dtype=i32, device=dev),
+                       torch.empty((G, E), dtype=f32, device=dev), torch.empty((G,), dtype=i32, device=dev))
+    if G == 0:                  # no tokens, no groups: nothing to address
+        return o
+    _check(load_library().prism_balance_loss(
+        ctypes.byref(desc), _typed(logits, f32, (T, E), "logits"), _typed(topk_idx, i32, (T, k), "topk_idx"),
+        _typed(token_mask, torch.uint8, (T,), "token_mask"), group_tokens, T, _typed(o.loss, f32, (G,), "loss"),
+        _typed(o.counts, i32, (G, E), "counts"), _typed(o.probs, f32, (G, E), "probs"),
+        _typed(o.n_tokens, i32, (G,), "n_tokens"), _ptr(workspace), workspace.numel(), _stream(stream)),
+        "prism_balance_loss")
+    return o
+
+
+def prism_route_backward(desc: LayerDesc, logits, topk_idx, balance: Optional[BalanceOut] = None, d_loss=None,
+                         d_gate=None, token_mask=None, group_tokens: int = 0, d_logits=None,
+                         stream=None) -> torch.Tensor:
+    """Gradient of sum(d_loss * balance.loss) + sum(d_gate * topk_gate) with respect to the logits (see prism.h)."""
+    T, E, k = logits.shape[0], desc.n_experts, desc.top_k
+    G = _balance_groups(T, group_tokens)
+    f32, i32 = torch.float32, torch.int32
+    if (balance is None) != (d_loss is None):
+        raise PrismError("d_loss comes with the balance it is the gradient of")
+    if d_logits is None:
+        d_logits = torch.empty((T, E), dtype=f32, device=logits.device)
+    if T == 0:
+        return d_logits
+    _check(load_library().prism_route_backward(
+        ctypes.byref(desc), _typed(logits, f32, (T, E), "logits"), _typed(topk_idx, i32, (T, k), "topk_idx"),
+        _typed(token_mask, torch.uint8, (T,), "token_mask"), group_tokens, T,
+        None if balance is None else _typed(balance.counts, i32, (G, E), "counts"),
+        None if balance is None else _typed(balance.n_tokens, i32, (G,), "n_tokens"),
+        _typed(d_loss, f32, (G,), "d_loss"), _typed(d_gate, f32, (T, k), "d_gate"),
+        _typed(d_logits, f32, (T, E), "d_logits"), _stream(stream)), "prism_route_backward")
+    return d_logits
+
+
 @dataclass
 class DispatchOut:
     local_src: torch.Tensor
@@ -205,7 +284,7 @@ def prism_dispatch(desc: LayerDesc, topk_idx, local_mask, workspace, stream=None
 
 def _clear_rows(desc: LayerDesc, offsets, n_rows, rows, stream) -> None:
     _check(load_library().prism_clear_rows(ctypes.byref(desc), _ptr(offsets), n_rows, _ptr(rows), _stream(stream)),
-           "prism_clear_rows")
+           "prism_clear_rows", "prism_balance_workspace_bytes", "prism_balance_loss", "prism_route_backward")
 
 
 def prism_expert_ffn(desc: LayerDesc, x, weights: WeightTable, local_src, local_offsets, workspace,

@@ -115,6 +115,45 @@ prism_status prism_route(const prism_layer_desc* desc, const void* x, const void
                       counts_accum, (hipStream_t)stream);
 }
 
+prism_status prism_balance_workspace_bytes(const prism_layer_desc* desc, size_t* bytes) {
+  PRISM_RETURN_IF(bytes == nullptr, PRISM_ERR_INVALID_ARG);
+  PRISM_TRY(validate_desc(desc, 0, false));
+  *bytes = balance_workspace_bytes(desc->n_experts);
+  return PRISM_OK;
+}
+
+prism_status prism_balance_loss(const prism_layer_desc* desc, const float* logits, const int32_t* topk_idx,
+                                const uint8_t* token_mask, int32_t group_tokens, int32_t T, float* loss,
+                                int32_t* counts, float* probs, int32_t* n_tokens, void* workspace,
+                                size_t workspace_bytes, void* stream) {
+  PRISM_ENTER();
+  PRISM_TRY(validate_desc(desc, T, false));
+  PRISM_RETURN_IF(group_tokens < 0, PRISM_ERR_INVALID_ARG);
+  PRISM_RETURN_IF(loss == nullptr || counts == nullptr || probs == nullptr || n_tokens == nullptr, PRISM_ERR_INVALID_ARG);
+  if (T > 0) PRISM_RETURN_IF(logits == nullptr || topk_idx == nullptr, PRISM_ERR_INVALID_ARG);
+  PRISM_RETURN_IF(workspace == nullptr || ((uintptr_t)workspace & 255u) != 0, PRISM_ERR_INVALID_ARG);
+  PRISM_RETURN_IF(workspace_bytes < balance_workspace_bytes(desc->n_experts), PRISM_ERR_WORKSPACE_TOO_SMALL);
+  return launch_balance(*desc, logits, topk_idx, token_mask, group_tokens, T, loss, counts, probs, n_tokens, workspace,
+                        (hipStream_t)stream);
+}
+
+prism_status prism_route_backward(const prism_layer_desc* desc, const float* logits, const int32_t* topk_idx,
+                                  const uint8_t* token_mask, int32_t group_tokens, int32_t T, const int32_t* counts,
+                                  const int32_t* n_tokens, const float* d_loss, const float* d_gate, float* d_logits,
+                                  void* stream) {
+  PRISM_ENTER();
+  PRISM_TRY(validate_desc(desc, T, false));
+  PRISM_RETURN_IF(group_tokens < 0, PRISM_ERR_INVALID_ARG);
+  PRISM_RETURN_IF((counts == nullptr) != (d_loss == nullptr) || (n_tokens == nullptr) != (d_loss == nullptr),
+                  PRISM_ERR_INVALID_ARG);
+  PRISM_RETURN_IF(d_loss == nullptr && d_gate == nullptr, PRISM_ERR_INVALID_ARG);
+  if (T > 0)
+    PRISM_RETURN_IF(logits == nullptr || d_logits == nullptr || (d_gate != nullptr && topk_idx == nullptr),
+                    PRISM_ERR_INVALID_ARG);
+  return launch_route_backward(*desc, logits, topk_idx, token_mask, group_tokens, T, counts, n_tokens, d_loss, d_gate,
+                               d_logits, (hipStream_t)stream);
+}
+
 prism_status prism_dispatch(const prism_layer_desc* desc, const int32_t* topk_idx,
                             const uint8_t* local_mask, int32_t T, int32_t* local_src,
                             int32_t* local_offsets, int32_t* remote_src, int32_t* remote_offsets,

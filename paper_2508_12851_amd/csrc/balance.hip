@@ -1,0 +1,412 @@
+// Balance loss of a batch's routing and the backward pass of the router (prism.h, prism_balance_loss and
+// prism_route_backward): what the activation counts f_n^l(e) of the paper's Sec. III-B are to a router that learns.
+//
+//   p[t, e]  = softmax(logits[t])             P[g, e] = mean of p[t, e] over the n tokens of group g that count
+//   loss[g]  = E / (k n) sum_e counts[g, e] P[g, e]
+//   d loss / d logits[t, e] = p[t, e] (u_e - sum_j u_j p[t, j]),   u_e = E counts[g, e] / (k n^2)
+//
+// A constant in all u_e drops out, so u is formed from E counts[e] - sum counts, a whole number: near an even spread the
+// counts themselves would cancel to a small difference in fp32.
+//
+// Rows: a token's E logits lie on 2^n lanes with 4 consecutive experts each, so that a wavefront holds one row of 256
+// experts or 64 rows of 4, and row sums are exchanges between lanes.  Both kernels read the logits once and are bound
+// by memory from a few MB on, by their launches below.
+#include <type_traits>
+
+#include "prism_internal.h"
+
+namespace prism {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+constexpr int kMaxE = PRISM_MAX_EXPERTS;
+
+struct RowArgs {
+  const float* logits;        // [T, E]
+  const int32_t* topk_idx;    // [T, k]
+  const uint8_t* mask;        // [T] or NULL
+  int T, E, k;
+  int group;                  // tokens of a group
+  int parts, part_rows;       // workgroups of a group and the tokens of each
+  bool vec;                   // rows can be moved 16 bytes at a time
+};
+
+// Tokens [first, end) of this workgroup: part blockIdx.x % parts of group blockIdx.x / parts.
+struct Rows {
+  int group, part, first, end;
+};
+__device__ __forceinline__ Rows rows_of(const RowArgs& a) {
+  const int g = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
+  const long long begin = (long long)g * a.group;     // (groups may be longer than the batch)
+  const int stop = (int)min(begin + a.group, (long long)a.T);
+  const int first = (int)min(begin + (long long)part * a.part_rows, (long long)stop);
+  return Rows{g, part, first, (int)min((long long)first + a.part_rows, (long long)stop)};
+}
+
+// The sum (or maximum) over the LPR lanes of a row, in all of them.
+template <int LPR, typename F> __device__ __forceinline__ float over_row(float v, F&& f) {
+  if constexpr (LPR > 1) v = f(v, row_xor<1>(v));
+  if constexpr (LPR > 2) v = f(v, row_xor<2>(v));
+  if constexpr (LPR > 4) v = f(v, row_xor<4>(v));
+  if constexpr (LPR > 8) v = f(v, row_xor<8>(v));
+  if constexpr (LPR > 16) v = f(v, __shfl_xor(v, 16));
+  if constexpr (LPR > 32) v = f(v, __shfl_xor(v, 32));
+  return v;
+}
+__device__ __forceinline__ float add(float a, float b) { return a + b; }
+
+// The 4 logits of this lane; experts past the last one have -inf.
+__device__ __forceinline__ f32x4 load_row(const RowArgs& a, int row, int e0) {
+  const float* p = a.logits + (size_t)row * a.E + e0;
+  f32x4 v = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+  if (a.vec) {
+    if (e0 < a.E) v = *reinterpret_cast<const f32x4*>(p);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (e0 + i < a.E) v[i] = p[i];
+  }
+  return v;
+}
+
+// softmax over the lanes of a row, in place.  Returns what turns a logit into its probability: {maximum, 1 / sum}.  An
+// expert at -inf has probability 0, and so have all of a row of nothing else.
+template <int LPR> __device__ __forceinline__ void softmax_row(f32x4& v) {
+  float m = over_row<LPR>(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), [](float x, float y) { return fmaxf(x, y); });
+  if (m == -INFINITY) m = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = expf(v[i] - m);
+  const float s = over_row<LPR>((v[0] + v[1]) + (v[2] + v[3]), add);
+  const float inv = s > 0.f ? 1.0f / s : s;     // (a NaN stays one)
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] *= inv;
+}
+
+// A group's results from its sums: probs, loss and the counts.  sum_p of expert threadIdx.x, in 64 bits; all threads call it.
+__device__ __forceinline__ void finish_group(int g, int E, int k, int n, int count, double sum_p, int32_t* counts, float* probs,
+                                             int32_t* n_tokens, float* loss) {
+  __shared__ double s_term[kThreads];
+  const int e = threadIdx.x;
+  double term = 0.0;
+  if (e < E) {
+    const double p = n > 0 ? sum_p / n : 0.0;
+    counts[(size_t)g * E + e] = count;
+    probs[(size_t)g * E + e] = (float)p;
+    term = (double)count * p;
+  }
+  s_term[e] = term;
+  for (int half = kThreads / 2; half > 0; half >>= 1) {
+    __syncthreads();
+    if (e < half) s_term[e] += s_term[e + half];
+  }
+  if (e == 0) {
+    n_tokens[g] = n;
+    loss[g] = n > 0 ? (float)(s_term[0] * E / ((double)k * n)) : 0.f;
+  }
+}
+
+static_assert(kThreads >= kMaxE, "a thread per expert");
+
+// Sums over a part of a group's tokens.  parts == 1: the group's results; else partial sums for finish_kernel: [workgroup]
+// {n, counts [E], probabilities [E]}.  A lane adds the probabilities of its experts over its rows in fp32 (16 of them where
+// 65536 tokens of 256 experts make 1024 parts), the wavefronts' sums are added in their order; the counts are whole
+// numbers, whose order does not matter.
+template <int LPR>
+__global__ __launch_bounds__(kThreads) void balance_kernel(const RowArgs a, int32_t* __restrict__ partial, int32_t* __restrict__ counts,
+                                                           float* __restrict__ probs, int32_t* __restrict__ n_tokens,
+                                                           float* __restrict__ loss) {
+  constexpr int kRows = 64 / LPR;           // rows a wavefront holds
+  constexpr int kAhead = LPR >= 16 ? 4 : 1; // ... and sets of them in flight
+  __shared__ int s_counts[kMaxE], s_n;
+  __shared__ f32x4 s_sum[kWaves][LPR];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const Rows r = rows_of(a);
+  s_counts[tid] = 0;
+  if (tid == 0) s_n = 0;
+  __syncthreads();
+  int live_rows = 0;
+  for (int row = r.first + tid; row < r.end; row += kThreads) live_rows += a.mask == nullptr || a.mask[row] != 0;
+  if (live_rows > 0) atomicAdd(&s_n, live_rows);
+  const long long picks = (long long)(r.end - r.first) * a.k;
+  for (long long i = tid; i < picks; i += kThreads) {
+    const int row = r.first + (int)(i / a.k);
+    const int e = a.topk_idx[(size_t)r.first * a.k + i];
+    if ((unsigned)e < (unsigned)a.E && (a.mask == nullptr || a.mask[row] != 0)) atomicAdd(&s_counts[e], 1);
+  }
+  const int e0 = (lane % LPR) * 4;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  for (int row0 = r.first + wave * kRows * kAhead; row0 < r.end; row0 += kWaves * kRows * kAhead) {
+    f32x4 v[kAhead];
+    bool live[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int row = row0 + u * kRows + lane / LPR;
+      live[u] = row < r.end && (a.mask == nullptr || a.mask[row] != 0);
+      v[u] = load_row(a, min(row, r.end - 1), e0);
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      softmax_row<LPR>(v[u]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum[i] += live[u] ? v[u][i] : 0.f;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {             // the rows of the wavefront
+    if constexpr (LPR <= 1) sum[i] += row_xor<1>(sum[i]);
+    if constexpr (LPR <= 2) sum[i] += row_xor<2>(sum[i]);
+    if constexpr (LPR <= 4) sum[i] += row_xor<4>(sum[i]);
+    if constexpr (LPR <= 8) sum[i] += row_xor<8>(sum[i]);
+    if constexpr (LPR <= 16) sum[i] += __shfl_xor(sum[i], 16);
+    if constexpr (LPR <= 32) sum[i] += __shfl_xor(sum[i], 32);
+  }
+  if (lane < LPR) s_sum[wave][lane] = sum;
+  __syncthreads();
+  float total = 0.f;
+  if (tid < a.E)
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) total += s_sum[w][tid / 4][tid % 4];
+  if (a.parts == 1) {
+    finish_group(r.group, a.E, a.k, s_n, s_counts[tid], total, counts, probs, n_tokens, loss);
+    return;
+  }
+  int32_t* out = partial + (size_t)blockIdx.x * (2 * a.E + 1);
+  if (tid == 0) out[0] = s_n;
+  if (tid < a.E) {
+    out[1 + tid] = s_counts[tid];
+    out[1 + a.E + tid] = __float_as_int(total);
+  }
+}
+
+// The parts of a group, added in 64 bits: thread (slice, expert) the parts slice, slice + slices, ..., then the slices.
+__global__ __launch_bounds__(kThreads) void finish_kernel(const int32_t* __restrict__ partial, int E, int k, int parts,
+                                                          int32_t* __restrict__ counts, float* __restrict__ probs,
+                                                          int32_t* __restrict__ n_tokens, float* __restrict__ loss) {
+  __shared__ double s_sum[kThreads];
+  __shared__ int s_count[kThreads], s_n[kThreads];
+  const int tid = threadIdx.x, g = blockIdx.x;
+  const int slices = kThreads / E;          // (1 to 256 experts)
+  const int slice = tid / E, e = tid - slice * E;
+  const int32_t* group = partial + (size_t)g * parts * (2 * E + 1);
+  double sum = 0.0;
+  int count = 0, n = 0;
+  if (slice < slices)
+#pragma unroll 4
+    for (int p = slice; p < parts; p += slices) {
+      const int32_t* in = group + (size_t)p * (2 * E + 1);
+      n += in[0];
+      count += in[1 + e];
+      sum += (double)__int_as_float(in[1 + E + e]);
+    }
+  s_sum[tid] = sum;
+  s_count[tid] = count;
+  s_n[tid] = n;
+  __syncthreads();
+  sum = 0.0;
+  count = n = 0;
+  for (int s = 0; s < slices; ++s) {
+    n += s_n[s * E];
+    if (tid < E) {
+      count += s_count[s * E + tid];
+      sum += s_sum[s * E + tid];
+    }
+  }
+  finish_group(g, E, k, n, count, sum, counts, probs, n_tokens, loss);
+}
+
+struct BackwardArgs {
+  RowArgs r;
+  const float* d_gate;        // [T, k] or NULL
+  const int32_t* counts;      // [G, E], with n_tokens and d_loss; or all NULL
+  const int32_t* n_tokens;
+  const float* d_loss;
+  float* d_logits;            // [T, E]
+  int softmax_all;
+};
+
+// Slot j of a row's picks belongs to lane j % LPR of the row, register j / LPR.
+template <int LPR> constexpr int slots_of = LPR >= PRISM_MAX_TOPK ? 1 : PRISM_MAX_TOPK / LPR;
+
+template <int LPR>
+__global__ __launch_bounds__(kThreads) void route_backward_kernel(const BackwardArgs b) {
+  constexpr int kRows = 64 / LPR, SL = slots_of<LPR>;
+  constexpr int kAhead = LPR >= 16 ? 2 : 1;
+  const RowArgs& a = b.r;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int in_row = lane % LPR, e0 = in_row * 4;
+  const Rows r = rows_of(a);
+  f32x4 u = {0.f, 0.f, 0.f, 0.f};           // d loss / d p of this lane's experts, up to a constant
+  if (b.counts != nullptr) {
+    const int n = b.n_tokens[r.group];
+    int c[4] = {0, 0, 0, 0}, all = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (e0 + i < a.E) c[i] = b.counts[(size_t)r.group * a.E + e0 + i];
+    all = c[0] + c[1] + c[2] + c[3];
+#pragma unroll
+    for (int off = 1; off < LPR; off <<= 1) all += __shfl_xor(all, off);
+    const double f = n > 0 ? (double)b.d_loss[r.group] / ((double)a.k * n * n) : 0.0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = (float)(f * (double)((long long)a.E * c[i] - all));
+  }
+  for (int row0 = r.first + wave * kRows * kAhead; row0 < r.end; row0 += kWaves * kRows * kAhead) {
+    f32x4 v[kAhead];
+    int idx[kAhead][SL];
+    float dg[kAhead][SL], l[kAhead][SL];
+    bool live[kAhead];
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s) {
+      const int row = min(row0 + s * kRows + lane / LPR, r.end - 1);
+      live[s] = a.mask == nullptr || a.mask[row] != 0;
+      v[s] = load_row(a, row, e0);
+#pragma unroll
+      for (int q = 0; q < SL; ++q) {
+        const int j = in_row + q * LPR;
+        idx[s][q] = -1;
+        dg[s][q] = 0.f;
+        if (b.d_gate != nullptr && j < a.k) {
+          idx[s][q] = a.topk_idx[(size_t)row * a.k + j];
+          if ((unsigned)idx[s][q] >= (unsigned)a.E) idx[s][q] = -1;
+          else dg[s][q] = b.d_gate[(size_t)row * a.k + j];
+        }
+        l[s][q] = idx[s][q] >= 0 && !b.softmax_all ? a.logits[(size_t)row * a.E + idx[s][q]] : -INFINITY;
+      }
+    }
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s) {
+      softmax_row<LPR>(v[s]);
+      // what the gates give: to u at a pick (softmax over all experts), or to the logit of a pick (over the picks)
+      float t[SL];
+      if (b.d_gate != nullptr && !b.softmax_all) {
+        float m = -INFINITY;
+#pragma unroll
+        for (int q = 0; q < SL; ++q) m = fmaxf(m, l[s][q]);
+        m = over_row<LPR>(m, [](float x, float y) { return fmaxf(x, y); });
+        if (m == -INFINITY) m = 0.f;
+        float sum = 0.f, dot = 0.f;
+#pragma unroll
+        for (int q = 0; q < SL; ++q) {
+          t[q] = expf(l[s][q] - m);
+          sum += t[q];
+          dot += t[q] * dg[s][q];
+        }
+        sum = over_row<LPR>(sum, add);
+        dot = over_row<LPR>(dot, add);
+        const float inv = sum > 0.f ? 1.0f / sum : sum;
+#pragma unroll
+        for (int q = 0; q < SL; ++q) t[q] = t[q] * inv * (dg[s][q] - dot * inv);
+      } else {
+#pragma unroll
+        for (int q = 0; q < SL; ++q) t[q] = dg[s][q];
+      }
+      f32x4 g = {0.f, 0.f, 0.f, 0.f};       // of this lane's experts
+      if (b.d_gate != nullptr)
+#pragma unroll
+        for (int j = 0; j < PRISM_MAX_TOPK; ++j) {
+          if (j >= a.k) break;
+          int e = idx[s][j / LPR];
+          float x = t[j / LPR];
+          if constexpr (LPR > 1) {
+            e = __shfl(e, j % LPR, LPR);
+            x = __shfl(x, j % LPR, LPR);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) g[i] += e == e0 + i ? x : 0.f;
+        }
+      f32x4 w = u;
+      if (b.softmax_all) w += g;
+      const float mean = over_row<LPR>((w[0] * v[s][0] + w[1] * v[s][1]) + (w[2] * v[s][2] + w[3] * v[s][3]), add);
+      f32x4 d;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        d[i] = v[s][i] * (w[i] - mean);
+        if (!b.softmax_all) d[i] += g[i];
+        if (!live[s]) d[i] = 0.f;           // whatever the row holds
+      }
+      const int row = row0 + s * kRows + lane / LPR;
+      if (row < r.end) {
+        float* out = b.d_logits + (size_t)row * a.E + e0;
+        if (a.vec) {
+          if (e0 < a.E) *reinterpret_cast<f32x4*>(out) = d;
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (e0 + i < a.E) out[i] = d[i];
+        }
+      }
+    }
+  }
+}
+
+// Calls fn with the number of lanes a row takes (a power of two, 4 experts on each).
+template <typename Fn> void with_lanes(int E, Fn&& fn) {
+  if (E <= 4) fn(std::integral_constant<int, 1>{});
+  else if (E <= 8) fn(std::integral_constant<int, 2>{});
+  else if (E <= 16) fn(std::integral_constant<int, 4>{});
+  else if (E <= 32) fn(std::integral_constant<int, 8>{});
+  else if (E <= 64) fn(std::integral_constant<int, 16>{});
+  else if (E <= 128) fn(std::integral_constant<int, 32>{});
+  else fn(std::integral_constant<int, 64>{});
+}
+
+constexpr int kBlocks = 1024;     // workgroups that a batch is cut into, about
+constexpr int kMaxGroups = PRISM_MAX_BALANCE_GROUPS;   // (a workgroup each: below 2^31 threads)
+constexpr int kFewRows = 16;      // rows per lane group and wavefront, at least
+
+// The groups of a batch, and how many workgroups share one.
+int split_groups(RowArgs* a, int group_tokens, int T, int max_parts_total) {
+  a->group = group_tokens > 0 ? group_tokens : std::max(T, 1);
+  const int G = group_tokens > 0 ? (int)(((long long)T + group_tokens - 1) / group_tokens) : 1;
+  int lanes = 1;
+  while (lanes * 4 < a->E) lanes *= 2;
+  const int rows_per_pass = kWaves * (64 / lanes);
+  const int rows = std::min(a->group, std::max(T, 1));
+  const int wanted = std::max(1, max_parts_total / std::max(G, 1));
+  a->part_rows = std::max(ceil_div(rows, wanted), rows_per_pass * kFewRows);
+  a->parts = ceil_div(rows, a->part_rows);
+  return G;
+}
+
+bool aligned16(const void* a, const void* b) { return (((uintptr_t)a | (uintptr_t)b) & 15u) == 0; }
+
+}  // namespace
+
+size_t balance_workspace_bytes(int E) { return align_up((size_t)kBlocks * (2 * E + 1) * 4, 256); }
+
+prism_status launch_balance(const prism_layer_desc& d, const float* logits, const int32_t* topk_idx, const uint8_t* mask,
+                            int group_tokens, int T, float* loss, int32_t* counts, float* probs, int32_t* n_tokens,
+                            void* workspace, hipStream_t st) {
+  RowArgs a{logits, topk_idx, mask, T, d.n_experts, d.top_k, 0, 1, 0, d.n_experts % 4 == 0 && aligned16(logits, nullptr)};
+  const int G = split_groups(&a, group_tokens, T, kBlocks);
+  if (G == 0) return PRISM_OK;
+  if (G > kMaxGroups) return PRISM_ERR_UNSUPPORTED;
+  with_lanes(a.E, [&](auto lanes) {
+    hipLaunchKernelGGL((balance_kernel<lanes.value>), dim3((unsigned)G * a.parts), dim3(kThreads), 0, st, a, (int32_t*)workspace,
+                       counts, probs, n_tokens, loss);
+  });
+  PRISM_CHECK_LAUNCH();
+  if (a.parts > 1) {
+    hipLaunchKernelGGL(finish_kernel, dim3((unsigned)G), dim3(kThreads), 0, st, (const int32_t*)workspace, a.E, a.k, a.parts,
+                       counts, probs, n_tokens, loss);
+    PRISM_CHECK_LAUNCH();
+  }
+  return PRISM_OK;
+}
+
+prism_status launch_route_backward(const prism_layer_desc& d, const float* logits, const int32_t* topk_idx, const uint8_t* mask,
+                                   int group_tokens, int T, const int32_t* counts, const int32_t* n_tokens, const float* d_loss,
+                                   const float* d_gate, float* d_logits, hipStream_t st) {
+  if (T == 0) return PRISM_OK;
+  BackwardArgs b{{logits, topk_idx, mask, T, d.n_experts, d.top_k, 0, 1, 0, d.n_experts % 4 == 0 && aligned16(logits, d_logits)},
+                 d_gate, counts, n_tokens, d_loss, d_logits, d.gate_mode == PRISM_GATES_SOFTMAX_ALL};
+  const int G = split_groups(&b.r, counts != nullptr ? group_tokens : 0, T, 2 * kBlocks);
+  if (G > kMaxGroups) return PRISM_ERR_UNSUPPORTED;
+  with_lanes(b.r.E, [&](auto lanes) {
+    hipLaunchKernelGGL((route_backward_kernel<lanes.value>), dim3((unsigned)G * b.r.parts), dim3(kThreads), 0, st, b);
+  });
+  PRISM_CHECK_LAUNCH();
+  return PRISM_OK;
+}
+
+}  // namespace prism

@@ -285,6 +285,16 @@ prism_status launch_pack_weights(const void* src, int rows, int cols, void* dst,
 prism_status launch_pack_rows(const prism_layer_desc& d, const void* x, const int32_t* src,
                               const int32_t* offsets, int T, void* packed, hipStream_t st);
 
+// Balance loss and router gradient (balance.hip); workspace: balance_workspace_bytes(E).
+size_t balance_workspace_bytes(int E);
+prism_status launch_balance(const prism_layer_desc& d, const float* logits, const int32_t* topk_idx, const uint8_t* mask,
+                            int group_tokens, int T, float* loss, int32_t* counts, float* probs, int32_t* n_tokens,
+                            void* workspace, hipStream_t st);
+// counts, n_tokens, d_loss: all or none; d_gate may be NULL.
+prism_status launch_route_backward(const prism_layer_desc& d, const float* logits, const int32_t* topk_idx, const uint8_t* mask,
+                                   int group_tokens, int T, const int32_t* counts, const int32_t* n_tokens, const float* d_loss,
+                                   const float* d_gate, float* d_logits, hipStream_t st);
+
 // ---------------------------------------------------------------------------
 // Device helpers.
 // ---------------------------------------------------------------------------
