@@ -284,7 +284,7 @@ def prism_dispatch(desc: LayerDesc, topk_idx, local_mask, workspace, stream=None
 
 def _clear_rows(desc: LayerDesc, offsets, n_rows, rows, stream) -> None:
     _check(load_library().prism_clear_rows(ctypes.byref(desc), _ptr(offsets), n_rows, _ptr(rows), _stream(stream)),
-           "prism_clear_rows", "prism_balance_workspace_bytes", "prism_balance_loss", "prism_route_backward")
+           "prism_clear_rows")
 
 
 def prism_expert_ffn(desc: LayerDesc, x, weights: WeightTable, local_src, local_offsets, workspace,
