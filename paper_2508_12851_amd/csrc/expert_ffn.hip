@@ -81,7 +81,7 @@ __global__ __launch_bounds__(256) void reduce_splits_kernel(const float* __restr
   const long long gid = (long long)blockIdx.x * blockDim.x + threadIdx.x;
   if (gid >= (long long)rows * vec_per_row) return;
   const int row = (int)(gid / vec_per_row);
-  if (row >= local_offsets[E] && row < A) return;   // rows that hold no assignment
+  if (row < A && (row < local_offsets[0] || row >= local_offsets[E])) return;   // rows that hold no assignment
   const int col = (int)(gid - (long long)row * vec_per_row) * 4;
   f32x4 v[kDecodeSplits];   // all slices asked for before the first is added
 #pragma unroll
@@ -158,7 +158,7 @@ __global__ __launch_bounds__(256) void pack_tokens_kernel(const uint4* __restric
                                                           int32_t* __restrict__ row_places) {
   const int lane = threadIdx.x & 63;
   const int r = blockIdx.x * 16 + (lane >> 2);
-  if (r >= rows || (r >= local_offsets[E] && r < A)) return;   // rows that hold no assignment
+  if (r >= rows || (r < A && (r < local_offsets[0] || r >= local_offsets[E]))) return;   // rows that hold no assignment
   const int tok = r < A ? local_src[r] / top_k : (r - A) % T;
   if (blockIdx.y == 0 && threadIdx.x < 64 && (lane & 3) == 0) row_places[r] = blockIdx.x * (H / 32) * 16 + (lane >> 2);
   const int tiles = H / 32, tile0 = (blockIdx.y * 4 + (threadIdx.x >> 6)) * 8;
