@@ -92,7 +92,23 @@ typedef enum {
  * prefill kernels consume 32 columns of a weight row at a time: from a row-major matrix that is
  * one half of a 128-byte cache line per row, and the L2 delivers the whole line both times;
  * from a tile, every line fetched is used completely.  Results are bit-identical. */
-typedef enum { PRISM_WEIGHTS_ROW_MAJOR = 0, PRISM_WEIGHTS_TILED = 1 } prism_weight_layout;
+typedef enum { PRISM_WEIGHTS_ROW_MAJOR = 0, PRISM_WEIGHTS_TILED = 1, PRISM_WEIGHTS_INT8 = 2 } prism_weight_layout;
+
+/* PRISM_WEIGHTS_INT8 (bf16 layers only): every expert weight matrix is an 8-bit matrix (below) made once, when the expert is
+ * loaded, by prism_quantize_i8 or prism_pack_i8: half the memory of a hosted expert, and half of what a migration moves.
+ * prism_expert_ffn and the whole-layer calls take them like the other layouts; prism_workspace_bytes asks for more.  With q(v) the
+ * row v in 8 bits and its scale:
+ *   y_a = (q(h) . Wq_down) s_h s_down,   h = silu(g) * u,   g = (q(x_t) . Wq_gate) s_x s_gate,   u likewise
+ * h is formed and quantised from fp32, sums of products are exact, y is rounded to bf16 once.  Results are a
+ * pure function of the inputs.  Limits: hidden and ffn at most 130944, and every operand in 8 bits ([T*k + S*T, max(H, F)]
+ * included) below 4 GiB.  Router, placement split, combine and the remote calls are those of the bf16 layer.
+ *
+ * 8-bit matrices.  [rows, cols] signed bytes with an fp32 scale per row, element (r, c) standing for byte * scale[r]: the bytes
+ * in tiles of 16 rows x 64 columns (1 KiB, row-tile major, rows of a tile 64 bytes apart), with R = rows rounded up to 16 and
+ * C = cols rounded up to 128 byte (r, c) lies at
+ *   ((r / 16) * (C / 64) + c / 64) * 1024 + (r % 16) * 64 + c % 64,
+ * zero for cols <= c < C and of no meaning for rows <= r < R; the scales lie at byte R * C, R of them.  prism_i8_bytes says how
+ * long all of it is; it must be 16-byte aligned. */
 
 /* Layer description: plain data in HOST memory, passed by const pointer. */
 typedef struct {
@@ -381,6 +397,33 @@ prism_status prism_moe_layer_traced(const prism_layer_desc* desc, const void* x,
  * PRISM_ERR_UNSUPPORTED (rows not a multiple of 16, cols not of 32, or the matrix is 4 GiB or more).
  */
 prism_status prism_pack_weights(const void* src, int32_t rows, int32_t cols, void* dst, void* stream);
+
+/*
+ * 8-bit matrices (see PRISM_WEIGHTS_INT8 above) and their product.
+ *
+ * prism_quantize_i8: rows of a matrix in 8 bits -- activations with a scale per token, or weights with one per output channel.
+ *   scale[r] = max |src[r]| * (1 / 127), both factors and the product in fp32;  byte = the integer nearest to src[r,c] / scale[r], exactly, ties to even, at
+ *   most 127 in magnitude.  A row of zeros has scale 0, one with a NaN or an infinity such a scale (and zeros).
+ *   src  [rows, cols] of prism_dtype src_dtype, ld elements from row to row; aligned to its elements
+ * prism_pack_i8: the same from bytes and scales that exist already (bytes are taken as they are, -128 too).
+ *   src  [rows, cols], ld bytes from row to row;  scale [rows]
+ * prism_matmul_i8: out[i,j] = (sum over l < k of a[i,l] b[j,l]) * scale_a[i] * scale_b[j], the sum exact, one rounding
+ *   at each product and one to out_dtype.  (Contractions that the library shares among workgroups: the fp32 values of up to 8 parts are added
+ *   in their order.)
+ *   a  [m,k], b [n,k] 8-bit matrices;  out [m,n] of prism_dtype out_dtype, ldo elements from row to row, of which only
+ *   the first n are written
+ *   workspace  256-byte aligned, prism_matmul_i8_workspace_bytes(max_m, n, k) for every m <= max_m
+ * Errors: INVALID_ARG (NULL, misaligned, sizes < 1, a row longer than ld), UNSUPPORTED (more than 130944 columns; a or b of 4 GiB or
+ * more in a product), WORKSPACE_TOO_SMALL.  No rows (m or rows of prism_quantize_i8 0) is PRISM_OK, with nothing launched.
+ */
+prism_status prism_i8_bytes(int32_t rows, int32_t cols, size_t* bytes);
+prism_status prism_quantize_i8(const void* src, int32_t src_dtype, int64_t ld, int32_t rows, int32_t cols, void* dst,
+                               void* stream);
+prism_status prism_pack_i8(const int8_t* src, int64_t ld, const float* scale, int32_t rows, int32_t cols, void* dst,
+                           void* stream);
+prism_status prism_matmul_i8_workspace_bytes(int32_t max_m, int32_t n, int32_t k, size_t* bytes);
+prism_status prism_matmul_i8(const void* a, const void* b, int32_t m, int32_t n, int32_t k, void* out, int64_t ldo,
+                             int32_t out_dtype, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Debug helper, NOT asynchronous: copies the pointer tables and the mask back

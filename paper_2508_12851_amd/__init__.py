@@ -10,4 +10,5 @@ from .binding import (  # noqa: F401
     prism_debug_check_weights, prism_pack_weights, prism_layer_permutation, LayerPermutation,
     prism_moe_layer_static, STATIC_SCRATCH_BYTES, prism_ceiling_hbm_read_pattern,
     BalanceOut, alloc_balance_workspace, prism_balance_loss, prism_route_backward,
+    I8Matrix, prism_quantize_i8, prism_pack_i8, prism_matmul_i8, alloc_matmul_i8_workspace,
 )

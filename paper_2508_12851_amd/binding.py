@@ -22,10 +22,11 @@ SYMBOLS = ("prism_status_string", "prism_workspace_bytes", "prism_route", "prism
            "prism_ceiling_mfma_bf16", "prism_ceiling_hbm_read", "prism_pack_remote",
            "prism_combine_remote", "prism_debug_check_weights", "prism_pack_weights",
            "prism_layer_permutation", "prism_moe_layer_static", "prism_ceiling_hbm_read_pattern",
-           "prism_clear_rows", "prism_balance_workspace_bytes", "prism_balance_loss", "prism_route_backward")
+           "prism_clear_rows", "prism_balance_workspace_bytes", "prism_balance_loss", "prism_route_backward",
+           "prism_i8_bytes", "prism_quantize_i8", "prism_pack_i8", "prism_matmul_i8_workspace_bytes", "prism_matmul_i8")
 STAGES = ("route", "dispatch", "ffn_up", "ffn_down", "combine")
 GATE_MODES = {"renormalized": 0, "softmax_all": 1}
-WEIGHT_LAYOUTS = {"row_major": 0, "tiled": 1}
+WEIGHT_LAYOUTS = {"row_major": 0, "tiled": 1, "int8": 2}
 
 
 class PrismError(RuntimeError):
@@ -69,6 +70,12 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.prism_balance_workspace_bytes.argtypes = [dp, ctypes.POINTER(sz)]
     lib.prism_balance_loss.argtypes = [dp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, sz, vp]
     lib.prism_route_backward.argtypes = [dp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp]
+    i64 = ctypes.c_int64
+    lib.prism_i8_bytes.argtypes = [i32, i32, ctypes.POINTER(sz)]
+    lib.prism_quantize_i8.argtypes = [vp, i32, i64, i32, i32, vp, vp]
+    lib.prism_pack_i8.argtypes = [vp, i64, vp, i32, i32, vp, vp]
+    lib.prism_matmul_i8_workspace_bytes.argtypes = [i32, i32, i32, ctypes.POINTER(sz)]
+    lib.prism_matmul_i8.argtypes = [vp, vp, i32, i32, i32, vp, i64, i32, vp, sz, vp]
     lib.prism_dispatch.argtypes = [dp, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.prism_expert_ffn.argtypes = [dp, vp, wp, vp, vp, i32, vp, vp, sz, vp]
     lib.prism_combine.argtypes = [dp, vp, vp, vp, vp, i32, vp, vp, sz, vp]
@@ -472,3 +479,86 @@ def prism_pack_weights(w, stream=None) -> torch.Tensor:
     _check(load_library().prism_pack_weights(_ptr(w), rows, cols, _ptr(packed), _stream(stream)),
            "prism_pack_weights")
     return packed
+
+
+@dataclass
+class I8Matrix:
+    """A matrix in 8 bits with a scale per row, in the library's layout (prism.h, "8-bit matrices")."""
+    data: torch.Tensor          # bytes
+    rows: int
+    cols: int
+
+    def values(self):
+        """(int8 [rows, cols], scales [rows]): copies in plain order."""
+        R, C = -(-self.rows // 16) * 16, -(-self.cols // 128) * 128
+        q = self.data[:R * C].view(torch.int8).view(R // 16, C // 64, 16, 64).permute(0, 2, 1, 3).reshape(R, C)
+        return (q[:self.rows, :self.cols].contiguous(),
+                self.data[R * C:R * C + 4 * self.rows].clone().view(torch.float32))
+
+
+def _alloc_i8(rows: int, cols: int, device) -> torch.Tensor:
+    n = ctypes.c_size_t(0)
+    if rows > 0:
+        _check(load_library().prism_i8_bytes(rows, cols, ctypes.byref(n)), "prism_i8_bytes")
+    return torch.empty(n.value, dtype=torch.uint8, device=device)
+
+
+def _rows_ptr(t: torch.Tensor, dtypes, what: str):
+    """(address, elements from row to row) of a matrix whose rows are contiguous."""
+    if t.dim() != 2 or t.dtype not in dtypes or not t.is_cuda:
+        raise PrismError(f"{what} has to be a device matrix of {' or '.join(map(str, dtypes))}")
+    if t.device.index != torch.cuda.current_device():
+        raise PrismError(f"{what} is on {t.device}, not on the current device")
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1 or rows > 1 and t.stride(0) < cols:
+        raise PrismError(f"{what} has to have contiguous rows that do not overlap")
+    return t.data_ptr(), t.stride(0) if rows > 1 else cols
+
+
+def _out_i8(out: Optional[I8Matrix], rows: int, cols: int, device) -> I8Matrix:
+    if out is None:
+        return I8Matrix(_alloc_i8(rows, cols, device), rows, cols)
+    if (out.rows, out.cols) != (rows, cols):
+        raise PrismError(f"out is an 8-bit matrix of {out.rows} x {out.cols}, not {rows} x {cols}")
+    return out
+
+
+def prism_quantize_i8(src, out: Optional[I8Matrix] = None, stream=None) -> I8Matrix:
+    """fp32 or bf16 rows -> 8 bits with a scale per row (see prism.h)."""
+    ptr, ld = _rows_ptr(src, (torch.float32, torch.bfloat16), "src")
+    rows, cols = src.shape
+    o = _out_i8(out, rows, cols, src.device)
+    _check(load_library().prism_quantize_i8(ptr, PRISM_F32 if src.dtype == torch.float32 else PRISM_BF16, ld, rows, cols,
+                                            _ptr(o.data), _stream(stream)), "prism_quantize_i8")
+    return o
+
+
+def prism_pack_i8(q, scale, out: Optional[I8Matrix] = None, stream=None) -> I8Matrix:
+    """int8 rows and their fp32 scales, as a checkpoint holds them -> the library's layout."""
+    ptr, ld = _rows_ptr(q, (torch.int8,), "q")
+    rows, cols = q.shape
+    o = _out_i8(out, rows, cols, q.device)
+    _check(load_library().prism_pack_i8(ptr, ld, _typed(scale, torch.float32, (rows,), "scale"), rows, cols, _ptr(o.data),
+                                        _stream(stream)), "prism_pack_i8")
+    return o
+
+
+def alloc_matmul_i8_workspace(max_m: int, n: int, k: int, device="cuda") -> torch.Tensor:
+    b = ctypes.c_size_t(0)
+    _check(load_library().prism_matmul_i8_workspace_bytes(max_m, n, k, ctypes.byref(b)), "prism_matmul_i8_workspace_bytes")
+    return torch.empty(b.value, dtype=torch.uint8, device=device)
+
+
+def prism_matmul_i8(a: I8Matrix, b: I8Matrix, workspace, out=None, dtype=torch.bfloat16, stream=None) -> torch.Tensor:
+    """a b^T of two 8-bit matrices [m, k] and [n, k]: [m, n] in bf16 or fp32."""
+    if a.cols != b.cols:
+        raise PrismError(f"rows of {a.cols} and of {b.cols} elements")
+    if out is None:
+        out = torch.empty((a.rows, b.rows), dtype=dtype, device=b.data.device)
+    if tuple(out.shape) != (a.rows, b.rows):
+        raise PrismError(f"out has to be {a.rows} x {b.rows}, not {tuple(out.shape)}")
+    ptr, ldo = _rows_ptr(out, (torch.float32, torch.bfloat16), "out")
+    _check(load_library().prism_matmul_i8(_ptr(a.data), _ptr(b.data), a.rows, b.rows, a.cols, ptr, ldo,
+                                          PRISM_F32 if out.dtype == torch.float32 else PRISM_BF16, _ptr(workspace),
+                                          workspace.numel(), _stream(stream)), "prism_matmul_i8")
+    return out

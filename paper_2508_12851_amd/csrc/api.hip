@@ -11,9 +11,10 @@ prism_status validate_desc(const prism_layer_desc* d, int32_t T, bool need_ffn_s
   PRISM_RETURN_IF(d->bias_group_tokens < 0, PRISM_ERR_INVALID_ARG);
   PRISM_RETURN_IF(d->gate_mode != PRISM_GATES_RENORMALIZED && d->gate_mode != PRISM_GATES_SOFTMAX_ALL,
                   PRISM_ERR_INVALID_ARG);
-  PRISM_RETURN_IF(d->weight_layout != PRISM_WEIGHTS_ROW_MAJOR && d->weight_layout != PRISM_WEIGHTS_TILED,
+  PRISM_RETURN_IF(d->weight_layout != PRISM_WEIGHTS_ROW_MAJOR && d->weight_layout != PRISM_WEIGHTS_TILED &&
+                      d->weight_layout != PRISM_WEIGHTS_INT8,
                   PRISM_ERR_INVALID_ARG);
-  PRISM_RETURN_IF(d->weight_layout == PRISM_WEIGHTS_TILED && d->dtype != PRISM_BF16, PRISM_ERR_UNSUPPORTED);
+  PRISM_RETURN_IF(d->weight_layout != PRISM_WEIGHTS_ROW_MAJOR && d->dtype != PRISM_BF16, PRISM_ERR_UNSUPPORTED);
   PRISM_RETURN_IF(d->dtype != PRISM_F32 && d->dtype != PRISM_BF16, PRISM_ERR_INVALID_ARG);
   PRISM_RETURN_IF(d->n_experts > PRISM_MAX_EXPERTS || d->top_k > PRISM_MAX_TOPK ||
                       d->n_shared > PRISM_MAX_SHARED,
@@ -25,6 +26,8 @@ prism_status validate_desc(const prism_layer_desc* d, int32_t T, bool need_ffn_s
     PRISM_RETURN_IF(d->ffn < 1, PRISM_ERR_INVALID_ARG);
     if (d->dtype == PRISM_BF16)
       PRISM_RETURN_IF(d->hidden % 64 != 0 || d->ffn % 64 != 0, PRISM_ERR_UNSUPPORTED);
+    if (d->weight_layout == PRISM_WEIGHTS_INT8)
+      PRISM_RETURN_IF(d->hidden > kI8MaxCols || d->ffn > kI8MaxCols, PRISM_ERR_UNSUPPORTED);
   }
   return PRISM_OK;
 }
@@ -48,6 +51,16 @@ static prism_status check_weights(const prism_layer_desc& d, const prism_expert_
                         w->shared_w_down == nullptr,
                     PRISM_ERR_INVALID_ARG);
   return PRISM_OK;
+}
+
+// The expert FFN on the buffers of a workspace, by the kind of its weights.
+static prism_status run_expert_ffn(const prism_layer_desc& d, const void* x, const prism_expert_weights& w,
+                                   const int32_t* local_src, const int32_t* local_offsets, int T, void* y, const Workspace& ws,
+                                   hipStream_t st, void* const* ev, const int32_t** deferred_splits, bool schedules_built) {
+  if (d.weight_layout == PRISM_WEIGHTS_INT8)
+    return launch_expert_ffn_i8(d, x, w, local_src, local_offsets, T, y, ws, st, ev, deferred_splits, schedules_built);
+  return launch_expert_ffn(d, x, w, local_src, local_offsets, T, y, ws.h, ws.h_tiled, ws.y, ws.tiles, ws.part, ws.slice_part,
+                           st, ev, deferred_splits, schedules_built);
 }
 
 // ---------------------------------------------------------------------------
@@ -185,8 +198,7 @@ prism_status prism_expert_ffn(const prism_layer_desc* desc, const void* x,
   if (T > 0) PRISM_RETURN_IF(x == nullptr || local_src == nullptr || y == nullptr, PRISM_ERR_INVALID_ARG);
   Workspace ws;
   PRISM_TRY(check_workspace(*desc, T, workspace, workspace_bytes, &ws));
-  return launch_expert_ffn(*desc, x, *weights, local_src, local_offsets, T, y, ws.h, ws.h_tiled, ws.y, ws.tiles,
-                           ws.part, ws.slice_part, (hipStream_t)stream, nullptr, nullptr);
+  return run_expert_ffn(*desc, x, *weights, local_src, local_offsets, T, y, ws, (hipStream_t)stream, nullptr, nullptr, false);
 }
 
 prism_status prism_combine(const prism_layer_desc* desc, const void* y, const int32_t* local_src,
@@ -247,6 +259,61 @@ prism_status prism_pack_weights(const void* src, int32_t rows, int32_t cols, voi
   PRISM_RETURN_IF(rows % 16 != 0 || cols % 32 != 0, PRISM_ERR_UNSUPPORTED);
   PRISM_RETURN_IF((size_t)rows * cols * 2 >= 0xFFFF0000ull, PRISM_ERR_UNSUPPORTED);
   return launch_pack_weights(src, rows, cols, dst, (hipStream_t)stream);
+}
+
+prism_status prism_i8_bytes(int32_t rows, int32_t cols, size_t* bytes) {
+  PRISM_RETURN_IF(bytes == nullptr || rows < 1 || cols < 1, PRISM_ERR_INVALID_ARG);
+  PRISM_RETURN_IF(cols > kI8MaxCols, PRISM_ERR_UNSUPPORTED);
+  *bytes = i8_bytes(rows, cols);
+  return PRISM_OK;
+}
+
+prism_status prism_quantize_i8(const void* src, int32_t src_dtype, int64_t ld, int32_t rows, int32_t cols, void* dst,
+                               void* stream) {
+  PRISM_ENTER();
+  PRISM_RETURN_IF(rows < 0 || cols < 1 || ld < cols, PRISM_ERR_INVALID_ARG);
+  PRISM_RETURN_IF(src_dtype != PRISM_F32 && src_dtype != PRISM_BF16, PRISM_ERR_INVALID_ARG);
+  PRISM_RETURN_IF(cols > kI8MaxCols, PRISM_ERR_UNSUPPORTED);
+  if (rows == 0) return PRISM_OK;
+  PRISM_RETURN_IF(src == nullptr || dst == nullptr || ((uintptr_t)dst & 15u) != 0, PRISM_ERR_INVALID_ARG);
+  PRISM_RETURN_IF((uintptr_t)src % (size_t)elem_size(src_dtype) != 0, PRISM_ERR_INVALID_ARG);
+  QuantizeArgs a{};
+  a.src = src; a.ld = ld; a.rows = rows; a.cols = cols;
+  a.dst = (uint8_t*)dst;
+  a.tiled = 1;
+  a.scale = (float*)((uint8_t*)dst + i8_elements(rows, cols));
+  return launch_quantize(a, src_dtype, (hipStream_t)stream);
+}
+
+prism_status prism_pack_i8(const int8_t* src, int64_t ld, const float* scale, int32_t rows, int32_t cols, void* dst,
+                           void* stream) {
+  PRISM_ENTER();
+  PRISM_RETURN_IF(rows < 1 || cols < 1 || ld < cols, PRISM_ERR_INVALID_ARG);
+  PRISM_RETURN_IF(cols > kI8MaxCols, PRISM_ERR_UNSUPPORTED);
+  PRISM_RETURN_IF(src == nullptr || scale == nullptr || dst == nullptr || ((uintptr_t)dst & 15u) != 0, PRISM_ERR_INVALID_ARG);
+  return launch_pack_i8(src, ld, scale, rows, cols, dst, (hipStream_t)stream);
+}
+
+prism_status prism_matmul_i8_workspace_bytes(int32_t max_m, int32_t n, int32_t k, size_t* bytes) {
+  PRISM_RETURN_IF(bytes == nullptr || max_m < 0 || n < 1 || k < 1, PRISM_ERR_INVALID_ARG);
+  PRISM_RETURN_IF(k > kI8MaxCols, PRISM_ERR_UNSUPPORTED);
+  *bytes = matmul_i8_workspace_bytes(max_m, n, k);
+  return PRISM_OK;
+}
+
+prism_status prism_matmul_i8(const void* a, const void* b, int32_t m, int32_t n, int32_t k, void* out, int64_t ldo,
+                             int32_t out_dtype, void* workspace, size_t workspace_bytes, void* stream) {
+  PRISM_ENTER();
+  PRISM_RETURN_IF(m < 0 || n < 1 || k < 1 || ldo < n, PRISM_ERR_INVALID_ARG);
+  PRISM_RETURN_IF(out_dtype != PRISM_F32 && out_dtype != PRISM_BF16, PRISM_ERR_INVALID_ARG);
+  PRISM_RETURN_IF(k > kI8MaxCols, PRISM_ERR_UNSUPPORTED);
+  if (m == 0) return PRISM_OK;
+  PRISM_RETURN_IF(a == nullptr || b == nullptr || out == nullptr || (((uintptr_t)a | (uintptr_t)b) & 15u) != 0,
+                  PRISM_ERR_INVALID_ARG);
+  PRISM_RETURN_IF((uintptr_t)out % (size_t)elem_size(out_dtype) != 0, PRISM_ERR_INVALID_ARG);
+  PRISM_RETURN_IF(workspace == nullptr || ((uintptr_t)workspace & 255u) != 0, PRISM_ERR_INVALID_ARG);
+  PRISM_RETURN_IF(workspace_bytes < matmul_i8_workspace_bytes(m, n, k), PRISM_ERR_WORKSPACE_TOO_SMALL);
+  return launch_matmul_i8(a, b, m, n, k, out, ldo, out_dtype, workspace, (hipStream_t)stream);
 }
 
 prism_status prism_debug_check_weights(const prism_layer_desc* desc,
@@ -314,15 +381,13 @@ prism_status prism_moe_layer_traced(const prism_layer_desc* desc, const void* x,
                                    remote_offsets, n_local_remote, remote_bytes, ws.inv, plan, counts,
                                    counts_accum, st, ws.tiles));
     trace(ev, PRISM_STAGE_DISPATCH, 1, st);
-    PRISM_TRY(launch_expert_ffn(*desc, x, *weights, ws.local_src, ws.local_offsets, T, ws.y, ws.h,
-                                ws.h_tiled, ws.y, ws.tiles, ws.part, ws.slice_part, st, ev, &n_splits, true));
+    PRISM_TRY(run_expert_ffn(*desc, x, *weights, ws.local_src, ws.local_offsets, T, ws.y, ws, st, ev, &n_splits, true));
   } else if (decode_front_end_applies(*desc, T)) {
     PRISM_TRY(launch_decode_front_end(*desc, x, w_router, router_bias, local_mask, T, topk_idx,
                                       topk_gate, counts, counts_accum, ws.local_src,
                                       ws.local_offsets, remote_src, remote_offsets, n_local_remote,
                                       remote_bytes, ws.inv, ws.route_part, ws.tiles, st, ev));
-    PRISM_TRY(launch_expert_ffn(*desc, x, *weights, ws.local_src, ws.local_offsets, T, ws.y, ws.h,
-                                ws.h_tiled, ws.y, ws.tiles, ws.part, ws.slice_part, st, ev, &n_splits, true));
+    PRISM_TRY(run_expert_ffn(*desc, x, *weights, ws.local_src, ws.local_offsets, T, ws.y, ws, st, ev, &n_splits, true));
   } else {
     trace(ev, PRISM_STAGE_ROUTE, 0, st);
     // the activation counts come out of the dispatch histogram, not out of the router
@@ -335,8 +400,7 @@ prism_status prism_moe_layer_traced(const prism_layer_desc* desc, const void* x,
                               remote_src, remote_offsets, n_local_remote, remote_bytes, ws.inv,
                               ws.block_hist, counts, counts_accum, st, ws.tiles, &schedules_built));
     trace(ev, PRISM_STAGE_DISPATCH, 1, st);
-    PRISM_TRY(launch_expert_ffn(*desc, x, *weights, ws.local_src, ws.local_offsets, T, ws.y, ws.h,
-                                ws.h_tiled, ws.y, ws.tiles, ws.part, ws.slice_part, st, ev, &n_splits, schedules_built));
+    PRISM_TRY(run_expert_ffn(*desc, x, *weights, ws.local_src, ws.local_offsets, T, ws.y, ws, st, ev, &n_splits, schedules_built));
   }
   trace(ev, PRISM_STAGE_COMBINE, 0, st);
   PRISM_TRY(launch_combine(*desc, ws.y, ws.inv, topk_gate, T, out, st, ws.part, n_splits));

@@ -12,63 +12,15 @@
 // bf16 path: the persistent grouped GEMM of grouped_gemm.h
 // (v_mfma_f32_32x32x16_bf16, 4 wavefronts per workgroup, operand k-tiles in an
 // LDS ring filled by direct-to-LDS loads), in the tile shapes chosen at the end
-// of this file.  GEMM1 loads the gate rows and the up rows of the same f range
+// of ffn_tiles.h.  GEMM1 loads the gate rows and the up rows of the same f range
 // into one tile, so silu(gate)*up is a register epilogue and only h is written.
 // Activation rows of GEMM1 are gathered through local_src; large batches of wide
 // layers first copy them in row order (pack_tokens_kernel).  Which tiles a batch
 // takes: ffn_paths.h.  fp32 layers: expert_ffn_f32.hip.
-#include "grouped_gemm.h"
-#include "prism_internal.h"
+#include "ffn_tiles.h"
 
 namespace prism {
 namespace {
-
-// ---------------------------------------------------------------------------
-// bf16 path: two grouped GEMMs on the matrix cores
-// ---------------------------------------------------------------------------
-template <int BM_, int BN_, int BK_, int STAGES_> struct TileCfg {
-  static constexpr int BM = BM_, BN = BN_, BK = BK_, STAGES = STAGES_;
-};
-
-// Fixed cost of one round of items of a split down projection, as weight bytes a workgroup
-// could have streamed meanwhile (first loads of the ring, epilogue, partial-tile stores): fitted
-// to the times of a 32-token batch of the 4096 x 14336 layer run with 2 to 8 splits.
-constexpr float kSplitRoundBytes = 14 * 8192.f;
-
-// Wide tiles of a path with two widths (schedule.h, "Two widths"): ring of their own, fewest items.
-constexpr int kWideStages = 3;
-constexpr int kWideItemsUp = 150, kWideItemsDown = 48;
-
-// What the schedule builders need to know about a path's two GEMMs (C1: gate/up, C2: down).
-template <typename C1, typename C2, bool SPLIT_DOWN, bool ROTATE, bool WIDTHS>
-FfnShapes shapes_of(const prism_layer_desc& d, int T) {
-  FfnShapes f{};
-  f.bm1 = C1::BM;
-  f.nt1 = ceil_div(d.ffn, C1::BN / 2);     // GEMM1 tile: BN/2 gate rows + BN/2 up rows
-  f.bm2 = C2::BM;
-  f.nt2 = ceil_div(d.hidden, C2::BN);
-  f.interleave = ROTATE;
-  // prefill tiles: the down projection's last round may be cut along its contraction
-  f.slice_kt2 = !SPLIT_DOWN && C2::BM == 256 && down_slicing_applies(d, T) ? d.ffn / C2::BK : 0;
-  if (SPLIT_DOWN) {
-    f.split_kt2 = d.ffn / C2::BK;
-    f.split_min_kt2 = C2::STAGES - 1;      // a slice must be at least as long as the k-tile ring
-    f.split_wgs2 = gg::gemm_wgs_per_xcd<C2::BM, C2::BN, 2, C2::BK, C2::STAGES, false, true>();
-    const float kt_bytes = (float)(C2::BN * C2::BK * 2);   // weight bytes of one k-tile
-    f.split_round_kt2 = kSplitRoundBytes / kt_bytes;
-    // one more split: every row written once more as fp32 and read once more, shared by all workgroups
-    f.split_row_kt2 = (float)d.hidden * 8.f / (float)(gg::kXcds * f.split_wgs2) / kt_bytes;
-  }
-  if (WIDTHS) {
-    static_assert(!WIDTHS || (SPLIT_DOWN && ROTATE && kWideStages <= C1::STAGES && kWideStages <= C2::STAGES),
-                  "the wide tiles' ring is no longer than the slices that the narrow ones allow");
-    f.wide_nt1 = ceil_div(d.ffn, C1::BN);
-    f.wide_nt2 = ceil_div(d.hidden, 2 * C2::BN);
-    f.wide_items1 = kWideItemsUp;
-    f.wide_items2 = kWideItemsDown;
-  }
-  return f;
-}
 
 // Sums the contraction slices of the split down projection: y = bf16(sum_s part[s]).
 __global__ __launch_bounds__(256) void reduce_splits_kernel(const float* __restrict__ part,
@@ -268,54 +220,35 @@ prism_status run_bf16_ffn(const prism_layer_desc& d, const void* x, const prism_
       PRISM_TRY((gg::launch_gemm<C2::BM, C2::BN, 2, 2, C2::BK, C2::STAGES, false, false, false, false, true>(
           g2, gg::sched_capacity(d, T, C2::BM, nt2), st)));
   }
-  if (slice_kt > 0) {
-    hipLaunchKernelGGL(sum_slices_kernel, dim3(gg::kXcds * (gg::kSliceSlots / 2) * kSumChunks), dim3(256), 0, st, sched2,
-                       gg::sched_capacity(d, T, C2::BM, nt2), slice_part, d.hidden, (uint16_t*)y);
-    PRISM_CHECK_LAUNCH();
-  }
-  if (SPLIT_DOWN && deferred_splits != nullptr) {
+  if (slice_kt > 0)
+    PRISM_TRY(launch_sum_slices(d, sched2, gg::sched_capacity(d, T, C2::BM, nt2), slice_part, y, st));
+  if (SPLIT_DOWN && deferred_splits != nullptr)
     *deferred_splits = n_splits;   // the caller's combine sums the slices itself
-  } else if (SPLIT_DOWN) {
-    const long long threads = (long long)rows * (d.hidden / 4);
-    hipLaunchKernelGGL(reduce_splits_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st,
-                       part, local_offsets, d.n_experts, A, rows, d.hidden, n_splits, (uint16_t*)y);
-    PRISM_CHECK_LAUNCH();
-  }
+  else if (SPLIT_DOWN)
+    PRISM_TRY(launch_reduce_splits(d, T, part, local_offsets, n_splits, y, st));
   trace(stage_events, PRISM_STAGE_FFN_DOWN, 1, st);
   return PRISM_OK;
 }
 
-// One tile path of the bf16 FFN: tile shapes of the two GEMMs, whether the down projection is
-// split along its contraction, whether the weight loads are marked non-temporal, whether the items
-// are dealt to the XCDs one by one with rotated contractions (grouped_gemm.h, ROTATE), whether the
-// schedule may choose tiles twice as wide instead.
-template <typename C1_, typename C2_, bool SPLIT_DOWN_, bool STREAM_B_, bool ROTATE_, bool WIDTHS_ = false> struct Path {
-  using C1 = C1_;
-  using C2 = C2_;
-  static constexpr bool kSplitDown = SPLIT_DOWN_, kStreamB = STREAM_B_, kRotate = ROTATE_, kWidths = WIDTHS_;
-};
+}  // namespace
 
-// Calls fn(Path<...>{}) with the path that serves a bf16 batch of T tokens of layer d (ffn_paths.h).
-template <typename Fn>
-auto select_path(const prism_layer_desc& d, int T, Fn&& fn) {
-  using Decode = TileCfg<64, 128, 64, 4>;
-  using Square = TileCfg<128, 128, 64, 4>;
-  using Wide = TileCfg<128, 256, 64, 3>;
-  switch (ffn_path(d, T)) {
-    case FfnPath::kDecodeTiled: return fn(Path<TileCfg<64, 128, 32, 8>, TileCfg<64, 128, 32, 8>, true, true, true>{});
-    case FfnPath::kDecode: return fn(Path<Decode, Decode, true, true, true>{});
-    case FfnPath::kDecodeShort: return fn(Path<TileCfg<64, 128, 32, 3>, TileCfg<64, 128, 32, 3>, true, true, true>{});
-    case FfnPath::kStream: return fn(Path<Square, Square, true, true, true, true>{});
-    case FfnPath::kSplitSquare: return fn(Path<Square, Square, true, false, false>{});
-    case FfnPath::kSplitWide: return fn(Path<Wide, Wide, true, false, false>{});
-    case FfnPath::kFewRows64: return fn(Path<Decode, Decode, false, true, false>{});
-    case FfnPath::kFewRows128: return fn(Path<Wide, Square, false, false, false>{});
-    case FfnPath::kPrefill: return fn(Path<TileCfg<256, 256, 32, 4>, TileCfg<256, 256, 32, 4>, false, false, false>{});
-    default: return fn(Path<TileCfg<256, 256, 32, 3>, TileCfg<256, 256, 32, 3>, false, false, false>{});
-  }
+prism_status launch_reduce_splits(const prism_layer_desc& d, int T, const float* part, const int32_t* local_offsets,
+                                  const int32_t* n_splits_ptr, void* y, hipStream_t st) {
+  const int A = T * d.top_k, rows = A + d.n_shared * T;
+  const long long threads = (long long)rows * (d.hidden / 4);
+  hipLaunchKernelGGL(reduce_splits_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, part, local_offsets,
+                     d.n_experts, A, rows, d.hidden, n_splits_ptr, (uint16_t*)y);
+  PRISM_CHECK_LAUNCH();
+  return PRISM_OK;
 }
 
-}  // namespace
+prism_status launch_sum_slices(const prism_layer_desc& d, const int32_t* sched, int capacity, const float* slice_part, void* y,
+                               hipStream_t st) {
+  hipLaunchKernelGGL(sum_slices_kernel, dim3(gg::kXcds * (gg::kSliceSlots / 2) * kSumChunks), dim3(256), 0, st, sched, capacity,
+                     slice_part, d.hidden, (uint16_t*)y);
+  PRISM_CHECK_LAUNCH();
+  return PRISM_OK;
+}
 
 prism_status launch_expert_ffn(const prism_layer_desc& d, const void* x,
                                const prism_expert_weights& w, const int32_t* local_src,

@@ -17,6 +17,14 @@ constexpr int kSquareMaxTokens = 448;   // up to this one in 128 x 128 tiles if 
 static inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 static inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
+// Length of a contraction of n elements as the tiles count it, in bf16 elements.  An 8-bit element is half of one, in rows
+// padded to 128 bytes (prism.h, "8-bit matrices"): a k-tile of as many bytes takes as many matrix instructions of the
+// same length, so that the rules of this file hold for 8-bit weights with the contraction counted so.
+constexpr int kI8RowAlign = 128;
+static inline int contraction(const prism_layer_desc& d, int n) {
+  return d.weight_layout == PRISM_WEIGHTS_INT8 ? (int)(align_up((size_t)n, kI8RowAlign) / 2) : n;
+}
+
 // Partial tiles of a down projection whose last round of work items is cut along the contraction:
 // one tile per workgroup.  Prefill batches of layers whose contraction is long enough for the cut
 // to pay: an item of K / 32 k-tiles takes about 0.74 us per k-tile, the cut saves at least half of
@@ -29,7 +37,7 @@ constexpr int kSliceMinFfn = 4096;
 // 400 tokens for instance, run in prefill tiles and are cut from here on.)
 constexpr int kSliceMinTokens = 353;
 static inline bool slicing_shape(const prism_layer_desc& d) {
-  return d.dtype == PRISM_BF16 && d.ffn >= kSliceMinFfn && d.hidden >= 128;
+  return d.dtype == PRISM_BF16 && contraction(d, d.ffn) >= kSliceMinFfn && contraction(d, d.hidden) >= 128;
 }
 static inline bool down_slicing_applies(const prism_layer_desc& d, int T) {
   return slicing_shape(d) && T >= kSliceMinTokens;
@@ -45,7 +53,8 @@ static inline int prefill_down_items(const prism_layer_desc& d, int T) {
 // Batches between the decode and the prefill sizes whose down projection in prefill tiles would
 // have too few items for the machine.  Layers of many small experts have enough at any batch size.
 static inline bool stream_tiles_apply(const prism_layer_desc& d, int T) {
-  if (T <= kDecodeMaxTokens || T > kStreamMaxTokens || d.hidden < 256 || d.ffn < 1024) return false;
+  if (T <= kDecodeMaxTokens || T > kStreamMaxTokens || contraction(d, d.hidden) < 256 || contraction(d, d.ffn) < 1024)
+    return false;
   return prefill_down_items(d, T) <= 128;
 }
 
@@ -57,7 +66,7 @@ constexpr int kFewRowsOnePick = 2560;    // most rows of a batch of one pick per
 constexpr int kVeryFewRows = 16;         // most rows per expert of the 64-row tiles
 constexpr int kVeryFewTokens = 1024;     // most tokens in them: an expert has at most that many rows
 static inline bool few_rows_per_expert(const prism_layer_desc& d, int T) {
-  if (T <= kDecodeMaxTokens || d.hidden < 192 || d.ffn < 192 || slicing_shape(d)) return false;
+  if (T <= kDecodeMaxTokens || contraction(d, d.hidden) < 192 || contraction(d, d.ffn) < 192 || slicing_shape(d)) return false;
   if (d.top_k == 1 && T > kFewRowsOnePick) return false;
   const int most = prefill_down_items(d, T) <= 256 ? kFewRowsFewItems : kFewRows;
   return (long long)T * d.top_k <= (long long)most * d.n_experts;
@@ -78,6 +87,7 @@ enum class FfnPath {
 
 // The path of a batch of T > 0 tokens of layer d (bf16).
 static inline FfnPath ffn_path(const prism_layer_desc& d, int T) {
+  const int k1 = contraction(d, d.hidden), k2 = contraction(d, d.ffn);
   if (T <= kDecodeMaxTokens) {
     // Decode batch: every expert has at most 64 rows, the layer is bound by streaming
     // the weights once.  Small tiles make ~1000 work items; the down projection also
@@ -90,9 +100,9 @@ static inline FfnPath ffn_path(const prism_layer_desc& d, int T) {
     // tile (with 64-wide k-tiles it would take halves of two), and twice the stages.
     // An expert has one row tile here, so every weight element is read by exactly one
     // workgroup, once: the weight loads are marked non-temporal (grouped_gemm.h, STREAM_B).
-    if (d.weight_layout == PRISM_WEIGHTS_TILED && d.hidden >= 256 && d.ffn >= 1024)
+    if (d.weight_layout != PRISM_WEIGHTS_ROW_MAJOR && k1 >= 256 && k2 >= 1024)
       return FfnPath::kDecodeTiled;
-    if (d.hidden >= 192 && d.ffn >= 192)
+    if (k1 >= 192 && k2 >= 192)
       return FfnPath::kDecode;
     return FfnPath::kDecodeShort;
   }
@@ -153,7 +163,7 @@ static inline FfnPath ffn_path(const prism_layer_desc& d, int T) {
   }
   // Prefill batch: 256 x 256 tiles (GEMM1: 128 gate + 128 up weight rows).  Very short
   // contractions (H or F of 64) get the shallowest ring.
-  if (d.hidden >= 128 && d.ffn >= 128)
+  if (k1 >= 128 && k2 >= 128)
     return FfnPath::kPrefill;
   return FfnPath::kPrefillShort;
 }
@@ -169,7 +179,7 @@ static inline FfnPath ffn_path(const prism_layer_desc& d, int T) {
 constexpr size_t kPackTiled = 22000000000, kPackRowMajor = 110000000000;
 static inline bool pack_rows_pays(const prism_layer_desc& d, int T) {
   const size_t rows = (size_t)T * (d.top_k + d.n_shared);
-  const size_t from = d.weight_layout == PRISM_WEIGHTS_TILED ? kPackTiled : kPackRowMajor;
+  const size_t from = d.weight_layout != PRISM_WEIGHTS_ROW_MAJOR ? kPackTiled : kPackRowMajor;
   // (the places lie behind the rows, in the partial sums' region: four fp32 rows per token and more)
   return slicing_shape(d) && T > kStreamMaxTokens && T <= 512 * d.hidden && rows * d.hidden * d.ffn >= from &&
          align_up(rows, 16) * d.hidden * 2 < 0xFFFF0000ull;

@@ -75,7 +75,22 @@ struct GemmArgs {
   uint32_t a_pitch;         // bytes from one source row of A to the next (GATED and a_tiled: 64)
   int a_kstep;              // bytes from 32 contraction elements of a row of A to the next 32
   int c_tiled;              // GATED: h is written in the same tiles ("Intermediate" below)
+  // 8-bit products ("8-bit integers" below).  K counts pairs of elements, h is fp32 and goes to Cpart.
+  const float* a_scale;     // a scale per row of A (GATED without a_tiled: per token)
+  const void* dense_b;      // DENSE: the one weight matrix; c_rows rows of A
+  void* dense_out;          // [c_rows, N] with dense_ldo elements from row to row
+  long long dense_ldo;
+  int dense_f32;            // fp32 instead of bf16
+  int dense_vec;            // rows can be stored 4 elements at a time
+  int dense_splits;         // SPLITK: workgroups that share an item
 };
+
+// 8-bit integers (I8).  A and the weights are matrices of signed bytes with a scale per row (prism.h, "8-bit matrices"), in
+// tiles of 16 rows x 64 bytes: to the loads, the ring and the LDS a row of K bytes is a row of K / 2 bf16 elements, and
+// v_mfma_i32_32x32x32_i8 takes 16 bytes per lane of both operands and as long as the bf16 instruction, for twice the
+// products.  (Which elements share a lane does not matter to a sum that takes both operands alike.)  The sums are exact in 32
+// bits; the epilogue multiplies them by the scales of their row and column in fp32.  The gate/up product leaves h in fp32: rounded
+// to bf16 before it is quantised, one in ten of its integers would be off by one.
 
 // Intermediate.  h is written by one of the two GEMMs and read by the other, so it lies in the order
 // that serves both: 16 x 32 tiles of 1 KiB over the absolute row number, like packed weights.  The
@@ -98,6 +113,8 @@ template <int WN, bool GATED, bool SPLITK> constexpr bool staged_store() {
 }
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+typedef int32_t i32x16 __attribute__((ext_vector_type(16)));
 
 // Schedule entries and pointer tables are written before the kernel starts and
 // never during it; reading them through the constant address space lets the
@@ -110,6 +127,29 @@ typedef const void* const __attribute__((address_space(4)))* const_ptr_table;
 // the result is rounded to bf16 right after).
 __device__ __forceinline__ float silu(float z) {
   return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896341f * z));
+}
+
+// Elements n .. n + 3 of a row of a dense product with N columns.
+__device__ __forceinline__ void store_dense(void* out, long long ldo, int f32, int vec, size_t row, int n, int N, const f32x4& v) {
+  if (f32) {
+    float* const p = (float*)out + row * (size_t)ldo + n;
+    if (vec && n + 4 <= N) {
+      *reinterpret_cast<f32x4*>(p) = v;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (n + e < N) p[e] = v[e];
+    }
+  } else {
+    bf16_t* const p = (bf16_t*)out + row * (size_t)ldo + n;
+    if (vec && n + 4 <= N) {
+      *reinterpret_cast<bf16x4*>(p) = bf16x4{(bf16_t)v[0], (bf16_t)v[1], (bf16_t)v[2], (bf16_t)v[3]};
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (n + e < N) p[e] = (bf16_t)v[e];
+    }
+  }
 }
 
 // LDS slot swizzle.  The LDS serves a 16-byte-per-lane read 16 lanes (256 bytes,
@@ -140,18 +180,20 @@ template <int BK> __device__ __forceinline__ int swizzle_key(int row) {
 // entry covers its own range of k-tiles and leaves its accumulators as an fp32 tile in slot
 // `part` of p.Cpart (plain GEMM only).  A launch of its own, so that the kernel that does the
 // bulk of the work carries none of this.
+// I8: 8-bit integers ("8-bit integers" above).  DENSE: one matrix product of c_rows rows with dense_b, no groups and no
+// schedule: the items are worked out from the sizes, in the order of the schedules' lists.
 template <int BM, int BN, int WGM, int WGN, int BK, int STAGES, bool GATED, bool SPLITK = false,
-          bool ROTATE = false, bool STREAM_B = false, bool SLICES = false>
+          bool ROTATE = false, bool STREAM_B = false, bool SLICES = false, bool I8 = false, bool DENSE = false>
 __global__ __launch_bounds__(kGemmThreads) void grouped_gemm_kernel(const GemmArgs p) {
 #include "grouped_gemm_body.h"
 }
 
 // The tiles the schedule chose (schedule.h, "Two widths"): BM x BN streamed, or BM x 2 BN in lists.  One launch
 // for both: a second one that ends at once would cost about 4 us.
-template <int BM, int NARROW, int BK, int NARROW_STAGES, int WIDE_STAGES, bool GATED, bool SPLITK>
+template <int BM, int NARROW, int BK, int NARROW_STAGES, int WIDE_STAGES, bool GATED, bool SPLITK, bool I8 = false>
 __global__ __launch_bounds__(kGemmThreads) void grouped_gemm_widths_kernel(const GemmArgs p) {
   constexpr int WGM = 2, WGN = 2;
-  constexpr bool SLICES = false;
+  constexpr bool SLICES = false, DENSE = false;
   if (((const_int_ptr)p.sched)[3] != 0) {
     constexpr int BN = 2 * NARROW, STAGES = WIDE_STAGES;
     constexpr bool ROTATE = false, STREAM_B = false;
@@ -179,31 +221,31 @@ static inline prism_status launch_build_schedules(const prism_layer_desc& d,
 }
 
 // LDS of one workgroup of a tile shape, and how many of them a CU holds.
-template <int BM, int BN, int WGN, int BK, int STAGES, bool GATED, bool SPLITK>
+template <int BM, int BN, int WGN, int BK, int STAGES, bool GATED, bool SPLITK, bool I8 = false>
 constexpr int gemm_lds_bytes() {
   return STAGES * (BM + BN) * BK * 2 + (GATED ? 4096 : 0) +           // ring + source-row slots
-         (staged_store<BN / WGN, GATED, SPLITK>() ? 4 * kStripBytes : 0);   // + strips
+         (!I8 && staged_store<BN / WGN, GATED, SPLITK>() ? 4 * kStripBytes : 0);   // + strips
 }
 constexpr int kCusPerXcd = 32;
-template <int BM, int BN, int WGN, int BK, int STAGES, bool GATED, bool SPLITK>
+template <int BM, int BN, int WGN, int BK, int STAGES, bool GATED, bool SPLITK, bool I8 = false>
 constexpr int gemm_wgs_per_xcd() {
-  return kCusPerXcd * ((160 * 1024) / gemm_lds_bytes<BM, BN, WGN, BK, STAGES, GATED, SPLITK>());
+  return kCusPerXcd * ((160 * 1024) / gemm_lds_bytes<BM, BN, WGN, BK, STAGES, GATED, SPLITK, I8>());
 }
 
 // capacity: items per XCD list (sched_capacity).  The grid holds as many workgroups
 // as fit on the machine at once (each then walks several items), or one per item.
 template <int BM, int BN, int WGM, int WGN, int BK, int STAGES, bool GATED, bool SPLITK = false,
-          bool ROTATE = false, bool STREAM_B = false, bool SLICES = false>
+          bool ROTATE = false, bool STREAM_B = false, bool SLICES = false, bool I8 = false, bool DENSE = false>
 prism_status launch_gemm(const GemmArgs& args, int capacity, hipStream_t st, int max_slots = 0) {
-  constexpr int smem = gemm_lds_bytes<BM, BN, WGN, BK, STAGES, GATED, SPLITK>();
+  constexpr int smem = gemm_lds_bytes<BM, BN, WGN, BK, STAGES, GATED, SPLITK, I8>();
   static_assert(smem <= 160 * 1024, "LDS per workgroup");
-  auto kernel = grouped_gemm_kernel<BM, BN, WGM, WGN, BK, STAGES, GATED, SPLITK, ROTATE, STREAM_B, SLICES>;
+  auto kernel = grouped_gemm_kernel<BM, BN, WGM, WGN, BK, STAGES, GATED, SPLITK, ROTATE, STREAM_B, SLICES, I8, DENSE>;
   static LdsLimitOnce lds_limit;   // one per instantiation
   if (!raise_lds_limit(lds_limit, (const void*)kernel, smem)) return PRISM_ERR_LAUNCH;
   if (capacity <= 0) return PRISM_OK;
   // persistent workgroups per XCD: as many as are resident at once (SPLITK: the schedule says
   // how they pair up, so the launch is never cut down to the list length)
-  int slots = gemm_wgs_per_xcd<BM, BN, WGN, BK, STAGES, GATED, SPLITK>();
+  int slots = gemm_wgs_per_xcd<BM, BN, WGN, BK, STAGES, GATED, SPLITK, I8>();
   if (max_slots > 0) slots = max_slots;
   if (!SPLITK && slots > capacity) slots = capacity;
   hipLaunchKernelGGL(kernel, dim3((unsigned)(slots * kXcds)), dim3(kGemmThreads), smem, st, args);
@@ -212,13 +254,13 @@ prism_status launch_gemm(const GemmArgs& args, int capacity, hipStream_t st, int
 }
 
 // The same for grouped_gemm_widths_kernel.
-template <int BM, int BN, int BK, int STAGES, int WIDE_STAGES, bool GATED, bool SPLITK>
+template <int BM, int BN, int BK, int STAGES, int WIDE_STAGES, bool GATED, bool SPLITK, bool I8 = false>
 prism_status launch_gemm_widths(const GemmArgs& args, hipStream_t st) {
-  constexpr int narrow = gemm_lds_bytes<BM, BN, 2, BK, STAGES, GATED, SPLITK>();
-  constexpr int wide = gemm_lds_bytes<BM, 2 * BN, 2, BK, WIDE_STAGES, GATED, SPLITK>();
+  constexpr int narrow = gemm_lds_bytes<BM, BN, 2, BK, STAGES, GATED, SPLITK, I8>();
+  constexpr int wide = gemm_lds_bytes<BM, 2 * BN, 2, BK, WIDE_STAGES, GATED, SPLITK, I8>();
   constexpr int smem = narrow > wide ? narrow : wide;
   static_assert(smem <= 160 * 1024 && smem > 80 * 1024, "one workgroup per CU");
-  auto kernel = grouped_gemm_widths_kernel<BM, BN, BK, STAGES, WIDE_STAGES, GATED, SPLITK>;
+  auto kernel = grouped_gemm_widths_kernel<BM, BN, BK, STAGES, WIDE_STAGES, GATED, SPLITK, I8>;
   static LdsLimitOnce lds_limit;   // one per instantiation
   if (!raise_lds_limit(lds_limit, (const void*)kernel, smem)) return PRISM_ERR_LAUNCH;
   hipLaunchKernelGGL(kernel, dim3(kCusPerXcd * kXcds), dim3(kGemmThreads), smem, st, args);

@@ -1,5 +1,5 @@
 // The body of the grouped GEMM kernels (grouped_gemm.h), for the tile BM x BN x BK, the ring of STAGES, the wavefront grid
-// WGM x WGN and the options GATED, SPLITK, ROTATE, STREAM_B, SLICES of the scope that includes it; p: its GemmArgs.  Text and
+// WGM x WGN and the options GATED, SPLITK, ROTATE, STREAM_B, SLICES, I8, DENSE of the scope that includes it; p: its GemmArgs.  Text and
 // not a function: as an inlined function of the arguments it compiles to other code in every kernel, 0.3 to 0.6 %
 // slower for decode batches.
 #if defined(__HIP_DEVICE_COMPILE__)   // buffer resources exist in device code only
@@ -10,6 +10,7 @@
   static_assert(MI >= 1 && NJ >= 1 && (!GATED || NJ % 2 == 0), "tile shape");
   static_assert(!(GATED && SPLITK), "the gated epilogue needs complete sums");
   static_assert(!SLICES || (!GATED && !SPLITK && !ROTATE), "slices are entries of the plain prefill GEMM");
+  static_assert(!DENSE || (I8 && !GATED && !SLICES), "one matrix instead of experts: 8-bit products");
   constexpr int kRowBytes = BK * 2;
   constexpr int CPR = BK / 8;                 // 16-byte chunks per LDS row
   constexpr int RPG = 1024 / kRowBytes;       // rows filled by one wavefront-wide 16-byte load
@@ -23,7 +24,7 @@
   static_assert((STAGES - 1) * LPS <= 63, "vmcnt is a 6-bit counter");
 
   // wide bf16 output tiles are stored through LDS strips (see the epilogue)
-  constexpr bool kStagedStore = staged_store<WN, GATED, SPLITK>();
+  constexpr bool kStagedStore = !I8 && staged_store<WN, GATED, SPLITK>();
   constexpr int kStripBase = STAGES * kStageBytes + (GATED ? 4096 : 0);
 
   extern __shared__ __align__(16) uint8_t smem[];
@@ -32,12 +33,16 @@
   const int xcd = blockIdx.x % kXcds;
   int slot = blockIdx.x / kXcds;
   const const_int_ptr sched_c = (const_int_ptr)p.sched;
-  const int count = sched_c[(SLICES ? 20 : 4) + xcd];
+  // DENSE: no schedule; every XCD takes an eighth of the sequence of items (schedule.h, "Work order")
+  const int dense_mt = DENSE ? (p.c_rows + BM - 1) / BM : 0, dense_nt = DENSE ? (p.N + BN - 1) / BN : 0;
+  const long long dense_items = (long long)dense_mt * dense_nt;
+  const int dense_first = DENSE ? (int)(dense_items * xcd / kXcds) : 0;
+  const int count = DENSE ? (int)(dense_items * (xcd + 1) / kXcds) - dense_first : sched_c[(SLICES ? 20 : 4) + xcd];
   int launched = gridDim.x / kXcds;
   // SPLITK: the schedule says how many workgroups share an item; neighbouring workgroups of an
   // XCD take the splits of one item slot, and those left over when the count does not divide the
   // launch end here.
-  const int n_splits = SPLITK ? max(sched_c[2], 1) : 1;
+  const int n_splits = SPLITK ? (DENSE ? p.dense_splits : max(sched_c[2], 1)) : 1;
   const int split = SPLITK ? slot % n_splits : 0;
   if (SPLITK) {
     slot /= n_splits;
@@ -54,7 +59,7 @@
   // slice entries sit in the last kSliceSlots places of every list
   const const_int4_ptr items =
       (const_int4_ptr)(p.sched + kSchedHeader) +
-      ((size_t)xcd * sched_c[1] + (SLICES ? sched_c[1] - kSliceSlots : 0)) * (kItemInts / 4);
+      (DENSE ? 0 : ((size_t)xcd * sched_c[1] + (SLICES ? sched_c[1] - kSliceSlots : 0)) * (kItemInts / 4));
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -88,6 +93,7 @@
   struct Ctx {
     int row_start, row_count, nt;
     int kt0, kt_n, part;     // as in Item
+    int tok_base;            // I8: as in Item
     int rot;                 // ROTATE: k-tile this item starts its contraction with
     const void* b0;
     const void* b1;
@@ -98,6 +104,14 @@
   const int n_ntiles = (p.N + (GATED ? BN / 2 : BN) - 1) / (GATED ? BN / 2 : BN);
   auto fetch_item = [&](int idx) {   // idx is clamped: the result is only used when idx < count
     const int i = min(idx, count - 1);
+    if (DENSE) {
+      // position / column tiles is a row tile of the part that the position lies in
+      const int seq = dense_first + i;
+      const PartOf rp = part_of(seq / dense_nt, dense_mt, kRectRows);
+      const int in_part = seq - rp.first * dense_nt;
+      const int nt = in_part / rp.len, row0 = (rp.first + in_part - nt * rp.len) * BM;
+      return Item{0, row0, min(BM, p.c_rows - row0), -1, nt, 0, KT, -1};
+    }
     if (ROTATE) {
       const unsigned seq = (unsigned)i * kXcds + (unsigned)xcd;
       const unsigned tile = seq / (unsigned)n_ntiles;
@@ -124,6 +138,7 @@
       __builtin_amdgcn_make_buffer_rsrc((void*)p.local_src, 0, (int)p.src_bytes, kBufferFlags);
   auto fetch_raw = [&](const Item& it) {
     Raw r;
+    if (DENSE) return Raw{p.dense_b, p.dense_b};
     const const_ptr_table t0 = (const_ptr_table)(it.g < p.E ? p.B0 : p.SB0);
     const const_ptr_table t1 = (const_ptr_table)(GATED ? (it.g < p.E ? p.B1 : p.SB1) : (it.g < p.E ? p.B0 : p.SB0));
     const int gi = it.g < p.E ? it.g : it.g - p.E;
@@ -156,6 +171,7 @@
     Ctx cx;
     cx.row_start = it.row_start; cx.row_count = it.row_count; cx.nt = it.nt;
     cx.kt0 = it.kt0; cx.kt_n = it.kt_n; cx.part = it.part;
+    cx.tok_base = it.tok_base;
     cx.rot = ROTATE ? (int)((unsigned)(it.nt * 13 + it.g * 29) % (unsigned)KT) : 0;
     cx.b0 = raw.b0; cx.b1 = raw.b1;
     // what depends on the lane is worked out anew per item: in registers across the k-loop it would push others out
@@ -187,7 +203,7 @@
       // GATED: tile rows [w WN, w WN + WN/2) are gate rows, the next WN/2 the up rows of the same f.  (N is a
       // multiple of 64: a group's rows all exist, or the last group stands in for it.)
       const int n = GATED ? it.nt * (BN / 2) + g0 / WN * (WN / 2) + g0 % WN % (WN / 2) : it.nt * BN + g0;
-      const uint32_t n0 = (uint32_t)min(n, p.N - RPG);
+      const uint32_t n0 = (uint32_t)min(n, (DENSE ? (p.N + 15) / 16 * 16 : p.N) - RPG);
       cx.b_voff[i] = (n0 >> 4) * block_bytes + (n0 & 15u) * b_pitch + b_lane;
     }
     return cx;
@@ -235,21 +251,23 @@
   const int b_off = (BM + wn * WN + r32) * kRowBytes;     // + 32 j rows
   const int key_r = swizzle_key<BK>(r32);
 
-  bf16x8 af[2][MI], bfr[2][NJ];
+  using frag_t = std::conditional_t<I8, i32x4, bf16x8>;     // 16 bytes of a row
+  using acc_t = std::conditional_t<I8, i32x16, f32x16>;
+  frag_t af[2][MI], bfr[2][NJ];
   auto read_frags = [&](int stage, int kk, int buf) {
     const uint8_t* base = smem + stage * kStageBytes;
     const int slot_b = ((kk * 2 + q) ^ key_r) * 16;
     // in the order the MFMAs below consume them
-    af[buf][0] = *reinterpret_cast<const bf16x8*>(base + a_off + slot_b);
+    af[buf][0] = *reinterpret_cast<const frag_t*>(base + a_off + slot_b);
 #pragma unroll
     for (int j = 0; j < NJ; ++j)
-      bfr[buf][j] = *reinterpret_cast<const bf16x8*>(base + b_off + j * 32 * kRowBytes + slot_b);
+      bfr[buf][j] = *reinterpret_cast<const frag_t*>(base + b_off + j * 32 * kRowBytes + slot_b);
 #pragma unroll
     for (int i = 1; i < MI; ++i)
-      af[buf][i] = *reinterpret_cast<const bf16x8*>(base + a_off + i * WGM * 32 * kRowBytes + slot_b);
+      af[buf][i] = *reinterpret_cast<const frag_t*>(base + a_off + i * WGM * 32 * kRowBytes + slot_b);
   };
 
-  f32x16 acc[MI][NJ];
+  acc_t acc[MI][NJ];
 
   // Ring protocol.  The k-tiles of this workgroup's items form one stream; stream
   // position g is computed from stage g % STAGES.  The prologue fills stages
@@ -265,7 +283,7 @@
   int fill_stage = STAGES - 1;         // (g + STAGES - 1) % STAGES
   // first: the first k-tile of an item, whose products start the sums (clearing the accumulators would take
   // as long as a k-tile's products, with nothing else to issue).
-  const f32x16 kZero = {};
+  const acc_t kZero = {};
   auto k_iteration = [&](const Ctx& fill_cx, int fill_kt, auto first) __attribute__((always_inline)) {
     const int next_stage = stage + 1 == STAGES ? 0 : stage + 1;
 #pragma unroll
@@ -288,8 +306,12 @@
           // snake order over the grid of accumulators: every MFMA shares an operand with the one
           // before it (0.5 % on the power-limited prefill GEMMs)
           const int j = (i & 1) ? NJ - 1 - j0 : j0;
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bfr[kk & 1][j], af[kk & 1][i],
+          if constexpr (I8)
+            acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(bfr[kk & 1][j], af[kk & 1][i],
                                                               first && kk == 0 ? kZero : acc[i][j], 0, 0, 0);
+          else
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bfr[kk & 1][j], af[kk & 1][i],
+                                                                first && kk == 0 ? kZero : acc[i][j], 0, 0, 0);
         }
       // Issue order inside the step: one MFMA first (so the wait for this step's
       // operands precedes any new LDS read), then the next step's operand reads one
@@ -405,7 +427,65 @@
       for (int w8 = 0; w8 < 8; ++w8) cur[w8] = nxt[w8];
     }
   };
+  // I8: sums of whole numbers times the scales of their row and column.  A weight matrix's scales lie behind its elements.
+  auto epilogue_i8 = [&](const Ctx& cx) {
+    const int n_tile = (GATED ? cx.nt * (BN / 2) + wn * (WN / 2) : cx.nt * BN + wn * WN) + q * 4;
+    const float* const s0 = reinterpret_cast<const float*>((const uint8_t*)cx.b0 + p.b_bytes);
+    const float* const s1 = reinterpret_cast<const float*>((const uint8_t*)cx.b1 + p.b_bytes);
+    constexpr int NO = GATED ? NJ / 2 : NJ;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      const int row = (i * WGM + wm) * 32 + r32;
+      if ((i * WGM + wm) * 32 >= cx.row_count) continue;      // wave-uniform
+      const int rr = min(row, cx.row_count - 1);
+      const size_t crow = (size_t)(cx.row_start + rr);
+      float rs;
+      if (GATED && !p.a_tiled) {                              // the token's scale
+        const uint32_t a = cx.tok_base >= 0 ? 0u : (uint32_t)p.local_src[crow];
+        rs = p.a_scale[cx.tok_base >= 0 ? (uint32_t)(cx.tok_base + rr) : k_magic != 0 ? __umulhi(a, k_magic) : a];
+      } else {
+        rs = p.a_scale[crow];
+      }
+      if (row >= cx.row_count) continue;
+#pragma unroll
+      for (int j = 0; j < NO; ++j)
+#pragma unroll
+        for (int vg = 0; vg < 4; ++vg) {
+          const int n = n_tile + j * 32 + vg * 8;
+          if (n >= p.N) continue;
+          f32x4 o;
+          if constexpr (GATED) {
+            const f32x4 c0 = *reinterpret_cast<const f32x4*>(s0 + n), c1 = *reinterpret_cast<const f32x4*>(s1 + n);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              o[e] = silu((float)acc[i][j][vg * 4 + e] * (rs * c0[e])) * ((float)acc[i][j + NO][vg * 4 + e] * (rs * c1[e]));
+            *reinterpret_cast<f32x4*>(p.Cpart + crow * p.N + n) = o;
+            continue;
+          }
+          const f32x4 c0 = *reinterpret_cast<const f32x4*>(s0 + n);   // (scales are padded to 16)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[e] = (float)acc[i][j][vg * 4 + e] * (rs * c0[e]);
+          if constexpr (SLICES) {
+            *reinterpret_cast<f32x4*>(p.Cpart + (size_t)cx.part * (BM * BN) + (size_t)row * BN + (n - cx.nt * BN)) = o;
+          } else if constexpr (SPLITK) {
+            float* const out = p.Cpart + ((size_t)split * p.c_rows + crow) * (DENSE ? (p.N + 3) / 4 * 4 : p.N) + n;
+            *reinterpret_cast<f32x4*>(out) = o;
+          } else if constexpr (DENSE) {
+            store_dense(p.dense_out, p.dense_ldo, p.dense_f32, p.dense_vec, crow, n, p.N, o);
+          } else {
+            bf16x4 b;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) b[e] = (bf16_t)o[e];
+            *reinterpret_cast<bf16x4*>(p.C + crow * p.N + n) = b;
+          }
+        }
+    }
+  };
   auto epilogue = [&](const Ctx& cx) {
+    if constexpr (I8) {
+      epilogue_i8(cx);
+      return;
+    } else {
     if constexpr (SLICES) {
       // the accumulators as they are, an fp32 tile [BM][BN] in slot cx.part
       float* tile = p.Cpart + (size_t)cx.part * (BM * BN);
@@ -473,6 +553,7 @@
             }
           }
       }
+    }
     }
   };
 

@@ -49,6 +49,10 @@ struct Workspace {
   float* slice_part;       // larger batches of wide layers: 256 partial tiles of 256 x 256 fp32 (cut last round of the down projection)
   double* route_part;      // decode batches: kRouteMaxHSplit partial sums of the logits, fp64, tokens and experts in tiles of 16
   bool h_tiled;            // h in 16 x 32 tiles (grouped_gemm.h, "Intermediate")
+  // 8-bit weights (h is fp32 then): the tokens and h in 8 bits, both with room for a row per row of h, and their scales
+  uint8_t *xq, *hq;        // [rows rounded up to 16][contraction in bytes]
+  float *x_scale, *h_scale;   // [rows]
+  int32_t* row_places;     // [rows] where a row's tokens lie in xq
   size_t total;
 };
 
@@ -87,11 +91,12 @@ static inline int max_splits(const prism_layer_desc& d, int T) {
 // prism_workspace_bytes() asks for; a buffer with room for the plain rows alone is served as well,
 // with h row-major.
 static inline Workspace carve(const prism_layer_desc& d, int T, void* base, bool tiled_h = true) {
-  Workspace w;
-  w.h_tiled = tiled_h && d.dtype == PRISM_BF16;
+  Workspace w{};
+  const bool i8 = d.weight_layout == PRISM_WEIGHTS_INT8;
+  w.h_tiled = tiled_h && d.dtype == PRISM_BF16 && !i8;
   const size_t A = (size_t)T * d.top_k;
   const size_t rows = A + (size_t)d.n_shared * T;
-  const size_t es = elem_size(d.dtype);
+  const size_t es = elem_size(d.dtype), h_es = i8 ? 4 : es;
   const int n_chunks = ceil_div((int)(A > 0 ? A : 1), kDispatchChunk);
   char* p = (char*)base;
   size_t off = 0;
@@ -101,7 +106,7 @@ static inline Workspace carve(const prism_layer_desc& d, int T, void* base, bool
   w.inv = (int32_t*)take(A * 4);
   w.block_hist = (int32_t*)take((size_t)n_chunks * d.n_experts * 4);
   w.tiles = (int32_t*)take(2 * tile_table_ints(d, T) * 4);
-  w.h = take((w.h_tiled ? align_up(rows, 16) : rows) * d.ffn * es);
+  w.h = take((w.h_tiled ? align_up(rows, 16) : rows) * d.ffn * h_es);
   w.y = take(rows * d.hidden * es);
   // The regions of the small-batch paths are reserved for every T (sized for min(T, limit of
   // the path) tokens), so that the total never shrinks as T grows: a workspace sized for
@@ -118,6 +123,13 @@ static inline Workspace carve(const prism_layer_desc& d, int T, void* base, bool
   w.slice_part = (float*)take(slice_part_bytes(d, T));
   w.route_part = (double*)take(bf16 ? (size_t)ceil_div((int)t_dec, kRouteTokTile) * kRouteMaxHSplit *
                                           route_col_tiles(d.n_experts) * 64 * 4 * 8 : 0);
+  if (i8) {
+    w.xq = (uint8_t*)take(align_up(rows, 16) * contraction(d, d.hidden) * 2);
+    w.hq = (uint8_t*)take(align_up(rows, 16) * contraction(d, d.ffn) * 2);
+    w.x_scale = (float*)take(rows * 4);
+    w.h_scale = (float*)take(rows * 4);
+    w.row_places = (int32_t*)take(rows * 4);
+  }
   w.total = off;
   return w;
 }
@@ -216,6 +228,47 @@ prism_status launch_expert_ffn(const prism_layer_desc& d, const void* x,
 prism_status launch_expert_ffn_f32(const prism_layer_desc& d, const void* x, const prism_expert_weights& w,
                                    const int32_t* local_src, const int32_t* local_offsets, int T, void* y,
                                    void* h, hipStream_t st, void* const* stage_events);
+
+// The 8-bit layers' part of launch_expert_ffn (T > 0).
+prism_status launch_expert_ffn_i8(const prism_layer_desc& d, const void* x, const prism_expert_weights& w,
+                                  const int32_t* local_src, const int32_t* local_offsets, int T, void* y, const Workspace& ws,
+                                  hipStream_t st, void* const* stage_events, const int32_t** deferred_splits,
+                                  bool schedules_built);
+// The sums of the contraction slices that a split or cut down projection left: *n_splits_ptr fp32 copies of all rows, or
+// the partial tiles of a cut last round (256 x 256).
+prism_status launch_reduce_splits(const prism_layer_desc& d, int T, const float* part, const int32_t* local_offsets,
+                                  const int32_t* n_splits_ptr, void* y, hipStream_t st);
+prism_status launch_sum_slices(const prism_layer_desc& d, const int32_t* sched, int capacity, const float* slice_part, void* y,
+                               hipStream_t st);
+
+// 8-bit matrices (prism.h): [rows rounded up to 16][cols rounded up to 128] bytes in tiles of 16 rows x 64, then a scale per row.
+static inline size_t i8_row_bytes(int cols) { return align_up((size_t)cols, kI8RowAlign); }
+static inline size_t i8_elements(int rows, int cols) { return align_up((size_t)rows, 16) * i8_row_bytes(cols); }
+static inline size_t i8_bytes(int rows, int cols) { return align_up(i8_elements(rows, cols) + align_up((size_t)rows, 16) * 4, 256); }
+constexpr int kI8MaxCols = 130944;      // 128 * 128 * this < 2^31: the sums of a product are exact in 32 bits
+
+// Rows in 8 bits, each with a scale: what the kernels of quantize_i8.hip are told.
+struct QuantizeArgs {
+  const void* src;           // rows of `cols` elements, ld elements apart
+  long long ld;
+  int rows, cols;
+  uint8_t* dst;
+  int tiled;                 // dst in tiles (prism.h), else rows of i8_row_bytes(cols) bytes
+  float* scale;              // [rows]
+  // A list of assignments: row r < A is the token local_src[r] / top_k (local_src NULL: row r itself), and of no use from
+  // local_offsets[E] on; row A + i is the token i mod T.  local_offsets NULL: all rows as they are.
+  const int32_t* local_src;
+  const int32_t* local_offsets;
+  int E, A, T, top_k;
+  int32_t* places;           // tiled: where each row starts in dst, in 64-byte units; or NULL
+};
+prism_status launch_quantize(const QuantizeArgs& a, int src_dtype, hipStream_t st);
+prism_status launch_pack_i8(const int8_t* src, long long ld, const float* scale, int rows, int cols, void* dst, hipStream_t st);
+
+// out = (a b^T) with the rows' scales (matmul_i8.hip).
+size_t matmul_i8_workspace_bytes(int max_rows, int N, int K);
+prism_status launch_matmul_i8(const void* a, const void* b, int M, int N, int K, void* out, long long ldo, int out_dtype,
+                              void* workspace, hipStream_t st);
 
 // True when launch_decode_front_end serves this layer shape and batch.
 bool decode_front_end_applies(const prism_layer_desc& d, int T);
