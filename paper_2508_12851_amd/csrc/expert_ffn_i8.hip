@@ -28,9 +28,9 @@ prism_status run_i8_ffn(const prism_layer_desc& d, const void* x, const prism_ex
   constexpr bool kPrefill = !SPLIT_DOWN && C2::BM == 256;
   if (!schedules_built) PRISM_TRY(gg::launch_build_schedules(d, local_offsets, T, ws.tiles, st));
 
-  // Prefill tiles read 64 bytes of a row per k-tile, half a line of a gathered one: their tokens are quantised in row order into
-  // tiles instead (once per pick).  Smaller batches gather.
-  const bool in_rows = kPrefill;
+  // Prefill tiles read 64 bytes of a row per k-tile, half a line of a gathered one: where a copy of the tokens in row order pays
+  // for bf16 weights, they are quantised in row order into tiles (once per pick).  Other batches gather.
+  const bool in_rows = kPrefill && pack_rows_pays(d, T);
   QuantizeArgs qx{};
   qx.src = x; qx.ld = d.hidden; qx.cols = d.hidden; qx.dst = ws.xq; qx.scale = ws.x_scale;
   qx.rows = T;
@@ -53,6 +53,7 @@ prism_status run_i8_ffn(const prism_layer_desc& d, const void* x, const prism_ex
   g1.K = k1; g1.N = d.ffn; g1.E = d.n_experts;
   g1.b_tiled = 1;
   g1.a_scale = ws.x_scale;
+  g1.a_scale_bytes = (uint32_t)(in_rows ? rows : T) * 4;
   if (in_rows) {
     g1.a_bytes = (uint32_t)i8_elements(rows, d.hidden);
     g1.local_src = ws.row_places;
@@ -100,6 +101,7 @@ prism_status run_i8_ffn(const prism_layer_desc& d, const void* x, const prism_ex
   g2.a_pitch = (uint32_t)k2 * 2;
   g2.a_kstep = 1024;
   g2.a_scale = ws.h_scale;
+  g2.a_scale_bytes = (uint32_t)rows * 4;
   const int32_t* n_splits = sched2 + 2;
   const int capacity2 = gg::sched_capacity(d, T, C2::BM, f.nt2);
   if constexpr (WIDTHS)

@@ -77,6 +77,7 @@ struct GemmArgs {
   int c_tiled;              // GATED: h is written in the same tiles ("Intermediate" below)
   // 8-bit products ("8-bit integers" below).  K counts pairs of elements, h is fp32 and goes to Cpart.
   const float* a_scale;     // a scale per row of A (GATED without a_tiled: per token)
+  uint32_t a_scale_bytes;
   const void* dense_b;      // DENSE: the one weight matrix; c_rows rows of A
   void* dense_out;          // [c_rows, N] with dense_ldo elements from row to row
   long long dense_ldo;
@@ -128,6 +129,13 @@ typedef const void* const __attribute__((address_space(4)))* const_ptr_table;
 __device__ __forceinline__ float silu(float z) {
   return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896341f * z));
 }
+
+// LDS floats of one wavefront for the scales of one item (I8): 64 per load.
+template <int WM, int WN, bool GATED> struct ScaleSlot {
+  static constexpr int kRowLoads = (WM + 63) / 64;
+  static constexpr int kColLoads = ((GATED ? WN / 2 : WN) + 63) / 64;   // of the gate and of the up columns, or of all
+  static constexpr int kBytes = (kRowLoads + (GATED ? 2 : 1) * kColLoads) * 256;
+};
 
 // Elements n .. n + 3 of a row of a dense product with N columns.
 __device__ __forceinline__ void store_dense(void* out, long long ldo, int f32, int vec, size_t row, int n, int N, const f32x4& v) {
@@ -221,9 +229,10 @@ static inline prism_status launch_build_schedules(const prism_layer_desc& d,
 }
 
 // LDS of one workgroup of a tile shape, and how many of them a CU holds.
+// (Four wavefronts, WGN of them side by side.)
 template <int BM, int BN, int WGN, int BK, int STAGES, bool GATED, bool SPLITK, bool I8 = false>
 constexpr int gemm_lds_bytes() {
-  return STAGES * (BM + BN) * BK * 2 + (GATED ? 4096 : 0) +           // ring + source-row slots
+  return (I8 ? 4 * 2 * ScaleSlot<BM * WGN / 4, BN / WGN, GATED>::kBytes : 0) + STAGES * (BM + BN) * BK * 2 + (GATED ? 4096 : 0) +           // ring + source-row slots
          (!I8 && staged_store<BN / WGN, GATED, SPLITK>() ? 4 * kStripBytes : 0);   // + strips
 }
 constexpr int kCusPerXcd = 32;

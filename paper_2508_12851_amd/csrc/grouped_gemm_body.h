@@ -26,6 +26,7 @@
   // wide bf16 output tiles are stored through LDS strips (see the epilogue)
   constexpr bool kStagedStore = !I8 && staged_store<WN, GATED, SPLITK>();
   constexpr int kStripBase = STAGES * kStageBytes + (GATED ? 4096 : 0);
+  constexpr int kScaleBase = kStripBase + (kStagedStore ? 4 * kStripBytes : 0);   // I8: see "scales" below
 
   extern __shared__ __align__(16) uint8_t smem[];
 
@@ -93,7 +94,6 @@
   struct Ctx {
     int row_start, row_count, nt;
     int kt0, kt_n, part;     // as in Item
-    int tok_base;            // I8: as in Item
     int rot;                 // ROTATE: k-tile this item starts its contraction with
     const void* b0;
     const void* b1;
@@ -171,7 +171,6 @@
     Ctx cx;
     cx.row_start = it.row_start; cx.row_count = it.row_count; cx.nt = it.nt;
     cx.kt0 = it.kt0; cx.kt_n = it.kt_n; cx.part = it.part;
-    cx.tok_base = it.tok_base;
     cx.rot = ROTATE ? (int)((unsigned)(it.nt * 13 + it.g * 29) % (unsigned)KT) : 0;
     cx.b0 = raw.b0; cx.b1 = raw.b1;
     // what depends on the lane is worked out anew per item: in registers across the k-loop it would push others out
@@ -207,6 +206,42 @@
       cx.b_voff[i] = (n0 >> 4) * block_bytes + (n0 & 15u) * b_pitch + b_lane;
     }
     return cx;
+  };
+
+  // I8, scales: those of an item's rows and columns as this wavefront's epilogue takes them, 4 bytes per lane and load into LDS, for the
+  // current item and the next.  They are asked for before the item's first k-tile and so have landed when it has.  (Loads into
+  // registers would wait for all k-tiles in flight, in the epilogue and, their registers being operands then, in the k-loop.)
+  // Row r32 of subtile i: float 32 i + r32; behind them column c of the wavefront (GATED: of the gate, then of the up columns).
+  using Slot = ScaleSlot<BM / WGM, BN / WGN, GATED>;
+  const uint32_t scale_slot = (uint32_t)(kScaleBase + wave * 2 * Slot::kBytes);
+  auto fetch_scales = [&](const Item& it, const Raw& raw, int parity) {
+    uint8_t* const slot_lds = smem + scale_slot + parity * Slot::kBytes;
+    int l = lane;
+    asm volatile("" : "+v"(l));
+    const __amdgpu_buffer_rsrc_t row_rsrc =
+        __builtin_amdgcn_make_buffer_rsrc((void*)p.a_scale, 0, (int)p.a_scale_bytes, kBufferFlags);
+#pragma unroll
+    for (int t = 0; t < Slot::kRowLoads; ++t) {
+      const int row = ((2 * t + (l >> 5)) * WGM + wm) * 32 + (l & 31);
+      uint32_t r = (uint32_t)(it.row_start + row);
+      if (GATED && !p.a_tiled) {   // the token's scale
+        const uint32_t a = reinterpret_cast<const uint32_t*>(src_lds)[min(row, it.row_count - 1)];
+        r = it.tok_base >= 0 ? (uint32_t)(it.tok_base + row) : k_magic != 0 ? __umulhi(a, k_magic) : a;
+      }
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(row_rsrc, (lds_ptr_t)(slot_lds + t * 256), 4,
+                                               row < it.row_count ? r * 4u : kOutOfRange, 0, 0, 0);
+    }
+    const int n0 = GATED ? it.nt * (BN / 2) + wn * (WN / 2) : it.nt * BN + wn * WN;
+#pragma unroll
+    for (int g = 0; g < (GATED ? 2 : 1); ++g) {
+      const __amdgpu_buffer_rsrc_t col_rsrc = __builtin_amdgcn_make_buffer_rsrc(
+          (void*)((const uint8_t*)(g == 0 ? raw.b0 : raw.b1) + p.b_bytes), 0, (p.N + 15) / 16 * 64, kBufferFlags);
+#pragma unroll
+      for (int t = 0; t < Slot::kColLoads; ++t)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(
+            col_rsrc, (lds_ptr_t)(slot_lds + (Slot::kRowLoads + g * Slot::kColLoads + t) * 256), 4,
+            (uint32_t)(n0 + t * 64 + l) * 4u, 0, 0, 0);
+    }
   };
 
   // Issues loads [first, last) of the LPS loads that fill one stage with k-tile kt
@@ -427,64 +462,57 @@
       for (int w8 = 0; w8 < 8; ++w8) cur[w8] = nxt[w8];
     }
   };
-  // I8: sums of whole numbers times the scales of their row and column.  A weight matrix's scales lie behind its elements.
-  auto epilogue_i8 = [&](const Ctx& cx) {
+  // I8: sums of whole numbers times the scales of their row and column.
+  auto epilogue_i8 = [&](const Ctx& cx, int parity) {
     const int n_tile = (GATED ? cx.nt * (BN / 2) + wn * (WN / 2) : cx.nt * BN + wn * WN) + q * 4;
-    const float* const s0 = reinterpret_cast<const float*>((const uint8_t*)cx.b0 + p.b_bytes);
-    const float* const s1 = reinterpret_cast<const float*>((const uint8_t*)cx.b1 + p.b_bytes);
+    const float* const scales = reinterpret_cast<const float*>(smem + scale_slot + parity * Slot::kBytes);
+    const float* const cols = scales + Slot::kRowLoads * 64 + q * 4;
     constexpr int NO = GATED ? NJ / 2 : NJ;
+    float rs[MI];
 #pragma unroll
-    for (int i = 0; i < MI; ++i) {
-      const int row = (i * WGM + wm) * 32 + r32;
-      if ((i * WGM + wm) * 32 >= cx.row_count) continue;      // wave-uniform
-      const int rr = min(row, cx.row_count - 1);
-      const size_t crow = (size_t)(cx.row_start + rr);
-      float rs;
-      if (GATED && !p.a_tiled) {                              // the token's scale
-        const uint32_t a = cx.tok_base >= 0 ? 0u : (uint32_t)p.local_src[crow];
-        rs = p.a_scale[cx.tok_base >= 0 ? (uint32_t)(cx.tok_base + rr) : k_magic != 0 ? __umulhi(a, k_magic) : a];
-      } else {
-        rs = p.a_scale[crow];
+    for (int i = 0; i < MI; ++i) rs[i] = scales[i * 32 + r32];
+#pragma unroll
+    for (int j = 0; j < NO; ++j) {
+      f32x4 c0[4], c1[4];
+#pragma unroll
+      for (int vg = 0; vg < 4; ++vg) {
+        c0[vg] = *reinterpret_cast<const f32x4*>(cols + j * 32 + vg * 8);
+        if (GATED) c1[vg] = *reinterpret_cast<const f32x4*>(cols + Slot::kColLoads * 64 + j * 32 + vg * 8);
       }
-      if (row >= cx.row_count) continue;
 #pragma unroll
-      for (int j = 0; j < NO; ++j)
+      for (int i = 0; i < MI; ++i) {
+        const int row = (i * WGM + wm) * 32 + r32;
+        if (row >= cx.row_count) continue;
+        const size_t crow = (size_t)(cx.row_start + row);
 #pragma unroll
         for (int vg = 0; vg < 4; ++vg) {
           const int n = n_tile + j * 32 + vg * 8;
           if (n >= p.N) continue;
           f32x4 o;
-          if constexpr (GATED) {
-            const f32x4 c0 = *reinterpret_cast<const f32x4*>(s0 + n), c1 = *reinterpret_cast<const f32x4*>(s1 + n);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              o[e] = silu((float)acc[i][j][vg * 4 + e] * (rs * c0[e])) * ((float)acc[i][j + NO][vg * 4 + e] * (rs * c1[e]));
-            *reinterpret_cast<f32x4*>(p.Cpart + crow * p.N + n) = o;
-            continue;
+          for (int e = 0; e < 4; ++e) {
+            o[e] = (float)acc[i][j][vg * 4 + e] * (rs[i] * c0[vg][e]);
+            if constexpr (GATED) o[e] = silu(o[e]) * ((float)acc[i][j + NO][vg * 4 + e] * (rs[i] * c1[vg][e]));
           }
-          const f32x4 c0 = *reinterpret_cast<const f32x4*>(s0 + n);   // (scales are padded to 16)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[e] = (float)acc[i][j][vg * 4 + e] * (rs * c0[e]);
-          if constexpr (SLICES) {
+          if constexpr (GATED) {
+            *reinterpret_cast<f32x4*>(p.Cpart + crow * p.N + n) = o;
+          } else if constexpr (SLICES) {
             *reinterpret_cast<f32x4*>(p.Cpart + (size_t)cx.part * (BM * BN) + (size_t)row * BN + (n - cx.nt * BN)) = o;
           } else if constexpr (SPLITK) {
-            float* const out = p.Cpart + ((size_t)split * p.c_rows + crow) * (DENSE ? (p.N + 3) / 4 * 4 : p.N) + n;
-            *reinterpret_cast<f32x4*>(out) = o;
+            *reinterpret_cast<f32x4*>(p.Cpart + ((size_t)split * p.c_rows + crow) * (DENSE ? (p.N + 3) / 4 * 4 : p.N) + n) = o;
           } else if constexpr (DENSE) {
             store_dense(p.dense_out, p.dense_ldo, p.dense_f32, p.dense_vec, crow, n, p.N, o);
           } else {
-            bf16x4 b;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) b[e] = (bf16_t)o[e];
-            *reinterpret_cast<bf16x4*>(p.C + crow * p.N + n) = b;
+            *reinterpret_cast<bf16x4*>(p.C + crow * p.N + n) =
+                bf16x4{(bf16_t)o[0], (bf16_t)o[1], (bf16_t)o[2], (bf16_t)o[3]};
           }
         }
+      }
     }
   };
-  auto epilogue = [&](const Ctx& cx) {
+  auto epilogue = [&](const Ctx& cx, int parity) {
     if constexpr (I8) {
-      epilogue_i8(cx);
-      return;
+      epilogue_i8(cx, parity);
     } else {
     if constexpr (SLICES) {
       // the accumulators as they are, an fp32 tile [BM][BN] in slot cx.part
@@ -565,6 +593,8 @@
   const Raw raw_cur = fetch_raw(it_cur);
   wait_vmcnt<0>();                       // the first item's source rows
   Ctx cur = make_ctx(it_cur, raw_cur);
+  int parity = 0;                        // I8: of the current item's scales
+  if constexpr (I8) fetch_scales(it_cur, raw_cur, 0);
   Item it_next = fetch_item(idx + slots);
 
 #pragma unroll
@@ -601,11 +631,13 @@
     // refills that already belong to the next item (for the last item: a harmless
     // re-fetch of this item's first k-tiles, which keeps the vmcnt bookkeeping uniform)
     const Ctx nxt = make_ctx(it_fill, raw_next);
+    if constexpr (I8) fetch_scales(it_fill, raw_next, parity ^ 1);
     for (int kt = max(kt_n - (STAGES - 1), 0); kt < kt_n; ++kt)
       k_iteration(nxt, min(kt + (STAGES - 1) - kt_n, (SLICES ? nxt.kt_n : KT) - 1), std::false_type{});
 
-    epilogue(cur);
+    epilogue(cur, parity);
     if (!has_next) break;
+    if constexpr (I8) parity ^= 1;
     cur = nxt;
     it_cur = it_next;
     it_next = it_next2;

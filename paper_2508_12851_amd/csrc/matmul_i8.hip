@@ -96,6 +96,7 @@ prism_status launch_matmul_i8(const void* a, const void* b, int M, int N, int K,
   g.a_tiled = g.b_tiled = 1;
   g.a_kstep = 1024;
   g.a_scale = (const float*)((const uint8_t*)a + i8_elements(M, K));
+  g.a_scale_bytes = (uint32_t)M * 4;
   g.dense_b = b;
   g.dense_out = out;
   g.dense_ldo = ldo;
