@@ -8,8 +8,8 @@
 // A value halfway between two integers is common, not rare: bf16 rows whose largest value has twice some element's
 // digits put that element at 63.5.
 //
-// Bound by memory: a workgroup takes a row, holds up to 16384 elements in registers between the maximum and the quotients, and reads
-// longer rows again.
+// Bound by memory: a wavefront or a workgroup takes a row and holds it in registers between the maximum and the quotients
+// (rows of more than 16384 elements are read again from there on).
 #include <type_traits>
 
 #include "prism_internal.h"
@@ -17,31 +17,54 @@
 namespace prism {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kElems = 8;                     // of a thread per pass
-constexpr int kHeld = 8;                      // passes whose elements stay in registers
+constexpr int kThreads = 256;                 // of pack_i8_kernel
+constexpr int kElems = 8;                     // of a lane per pass
 constexpr int kMaxGrid = 1 << 20;             // workgroups (a grid has fewer than 2^32 threads)
 
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
+// 8 elements of a row.  grow(m): m joined with the largest |v|; bits_of(m): that as the bits of a float, in which a NaN
+// is larger than all numbers.
 template <typename S> struct Chunk;
 template <> struct Chunk<float> {
+  typedef uint32_t Max;
   f32x4 a, b;
   __device__ void load(const float* p) {
     a = reinterpret_cast<const f32x4*>(p)[0];
     b = reinterpret_cast<const f32x4*>(p)[1];
   }
   __device__ void set(int i, float v) { (i < 4 ? a : b)[i & 3] = v; }
-  __device__ float get(int i) const { return (i < 4 ? a : b)[i & 3]; }
+  __device__ __forceinline__ float get(int i) const { return (i < 4 ? a : b)[i & 3]; }
+  __device__ __forceinline__ void grow(Max& m) const {
+#pragma unroll
+    for (int i = 0; i < kElems; ++i) m = max(m, __float_as_uint(get(i)) & 0x7fffffffu);
+  }
+  static __device__ __forceinline__ uint32_t bits_of(Max m) { return m; }
 };
 template <> struct Chunk<bf16_t> {
-  bf16x8 a;
-  __device__ void load(const bf16_t* p) { a = *reinterpret_cast<const bf16x8*>(p); }
-  __device__ void set(int i, bf16_t v) { a[i] = v; }
-  __device__ float get(int i) const { return (float)a[i]; }
+  typedef u16x2 Max;
+  uint4 a;
+  __device__ void load(const bf16_t* p) { a = *reinterpret_cast<const uint4*>(p); }
+  __device__ void set(int i, bf16_t v) {
+    uint32_t& w = i < 2 ? a.x : i < 4 ? a.y : i < 6 ? a.z : a.w;
+    const uint32_t b = __builtin_bit_cast(uint16_t, v);
+    w = i & 1 ? (w & 0xffffu) | b << 16 : (w & 0xffff0000u) | b;
+  }
+  __device__ __forceinline__ float get(int i) const {
+    const uint32_t w = i < 2 ? a.x : i < 4 ? a.y : i < 6 ? a.z : a.w;
+    return i & 1 ? bf16_hi(w) : bf16_lo(w);
+  }
+  __device__ __forceinline__ void grow(Max& m) const {
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w[i] & 0x7fff7fffu));
+  }
+  static __device__ __forceinline__ uint32_t bits_of(Max m) { return (uint32_t)max(m.x, m.y) << 16; }
 };
 
 // Elements c .. c + 7 of a row of n, zeros past its end.
 template <typename S, bool VEC> __device__ __forceinline__ Chunk<S> load_chunk(const S* row, int c, int n) {
-  Chunk<S> v;
+  Chunk<S> v{};
   if (VEC && c + kElems <= n) {
     v.load(row + c);
   } else {
@@ -51,21 +74,15 @@ template <typename S, bool VEC> __device__ __forceinline__ Chunk<S> load_chunk(c
   return v;
 }
 
-// |v| of the largest as its bits, in which a NaN is larger than all numbers.
-template <typename S> __device__ __forceinline__ uint32_t grow(uint32_t m, const Chunk<S>& v) {
-#pragma unroll
-  for (int i = 0; i < kElems; ++i) m = max(m, __float_as_uint(v.get(i)) & 0x7fffffffu);
-  return m;
-}
-
+// v / scale to the nearest integer, exactly.  scale and values are lifted where the reciprocal would not be finite.
 struct Quotient {
-  float scale, inverse, lift;     // scale and values are lifted where the reciprocal would not be finite
+  float scale, inverse, lift;
   __device__ explicit Quotient(float s) {
     lift = s < 0x1p-64f ? 0x1p64f : 1.f;
     scale = s * lift;
     inverse = 1.0f / scale;
   }
-  __device__ __forceinline__ int operator()(float v) const {
+  __device__ __forceinline__ int exact(float v) const {
     v *= lift;
     float q = rintf(v * inverse);
     const float r2 = 2.f * fmaf(-q, scale, v);
@@ -75,14 +92,28 @@ struct Quotient {
     return (int)fminf(fmaxf(q, -127.f), 127.f);
   }
 };
+// The 8 bytes of a chunk.  v * inverse is off by at most 127.5 * 2^-24 from the quotient (its factor's rounding; the product is
+// not rounded before 1.5 * 2^23 is added, which leaves the integer in the low bits), so that only a chunk with a
+// product within 10^-4 of a half needs the exact look: one in a hundred of random values.
+constexpr float kRound = 12582912.f;
 template <typename S> __device__ __forceinline__ uint2 quotients(const Chunk<S>& v, const Quotient& q) {
+  uint32_t b[kElems];
+  float far = 0.f;
+#pragma unroll
+  for (int i = 0; i < kElems; ++i) {
+    const float x = v.get(i), t = fmaf(x, q.inverse, kRound);
+    b[i] = __float_as_uint(t);
+    far = fmaxf(far, fabsf(fmaf(x, q.inverse, kRound - t)));
+  }
+  if (far > 0.4999f || q.lift != 1.f) {
+#pragma unroll
+    for (int i = 0; i < kElems; ++i) b[i] = (uint32_t)q.exact(v.get(i));
+  }
   uint32_t w[2];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    w[h] = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[h] |= (uint32_t)(q(v.get(4 * h + i)) & 0xff) << (8 * i);
-  }
+  for (int h = 0; h < 2; ++h)
+    w[h] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[4 * h + 3], b[4 * h + 2], 0x0c0c0400u),
+                                 __builtin_amdgcn_perm(b[4 * h + 1], b[4 * h], 0x0c0c0400u), 0x05040100u);
   return uint2{w[0], w[1]};
 }
 
@@ -91,8 +122,9 @@ __device__ __forceinline__ size_t byte_of(int r, int c, size_t row_bytes, bool t
   return tiled ? ((size_t)(r >> 4) * (row_bytes / 64) + (c >> 6)) * 1024 + (r & 15) * 64 + (c & 63) : (size_t)r * row_bytes + c;
 }
 
-template <typename S, bool VEC> __device__ __forceinline__ void quantize_row(const QuantizeArgs& a, int r) {
-  __shared__ uint32_t s_max[kThreads / 64];
+// Row r on LANES lanes (a wavefront, or a workgroup), `lane` of them this one.
+template <typename S, bool VEC, int LANES, int HELD>
+__device__ __forceinline__ void quantize_row(const QuantizeArgs& a, int r, int lane) {
   int from = r;
   if (a.local_offsets != nullptr) {
     if (r < a.A && (r < a.local_offsets[0] || r >= a.local_offsets[a.E])) return;   // holds no assignment
@@ -100,48 +132,57 @@ template <typename S, bool VEC> __device__ __forceinline__ void quantize_row(con
   }
   const S* row = (const S*)a.src + (size_t)from * a.ld;
   const int row_bytes = (a.cols + kI8RowAlign - 1) / kI8RowAlign * kI8RowAlign;
-  const int c0 = threadIdx.x * kElems;
-  constexpr int kPass = kThreads * kElems;
-  Chunk<S> held[kHeld];
-  uint32_t m = 0;
+  const int c0 = lane * kElems;
+  constexpr int kPass = LANES * kElems;
+  Chunk<S> held[HELD];
+  typename Chunk<S>::Max grown{};
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i)
+  for (int i = 0; i < HELD; ++i)
     if (c0 + i * kPass < a.cols) held[i] = load_chunk<S, VEC>(row, c0 + i * kPass, a.cols);
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i)
-    if (c0 + i * kPass < a.cols) m = grow(m, held[i]);
-  for (int c = c0 + kHeld * kPass; c < a.cols; c += kPass) m = grow(m, load_chunk<S, VEC>(row, c, a.cols));
+  for (int i = 0; i < HELD; ++i)
+    if (c0 + i * kPass < a.cols) held[i].grow(grown);
+  for (int c = c0 + HELD * kPass; c < a.cols; c += kPass) load_chunk<S, VEC>(row, c, a.cols).grow(grown);
+  uint32_t m = Chunk<S>::bits_of(grown);
+  m = max(m, (uint32_t)row_xor<1>((int)m));
+  m = max(m, (uint32_t)row_xor<2>((int)m));
+  m = max(m, (uint32_t)row_xor<4>((int)m));
+  m = max(m, (uint32_t)row_xor<8>((int)m));
+  m = max(m, (uint32_t)__shfl_xor((int)m, 16));
+  m = max(m, (uint32_t)__shfl_xor((int)m, 32));
+  if constexpr (LANES > 64) {
+    __shared__ uint32_t s_max[LANES / 64];
+    lds_barrier();                            // (the row before has been read)
+    if ((lane & 63) == 0) s_max[lane >> 6] = m;
+    lds_barrier();
+    m = s_max[0];
 #pragma unroll
-  for (int off = 32; off > 0; off >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, off));
-  if ((threadIdx.x & 63) == 0) s_max[threadIdx.x >> 6] = m;
-  __syncthreads();
-  m = max(max(s_max[0], s_max[1]), max(s_max[2], s_max[3]));
+    for (int w = 1; w < LANES / 64; ++w) m = max(m, s_max[w]);
+  }
   const float scale = __uint_as_float(m) * (1.f / 127.f);
-  if (threadIdx.x == 0) {
+  if (lane == 0) {
     a.scale[r] = scale;
     if (a.places != nullptr) a.places[r] = (r >> 4) * (row_bytes / 64) * 16 + (r & 15);
   }
-  const Quotient q(scale > 0.f ? scale : 1.f);     // (a row of zeros; of one that is not finite only the scale says so)
-  uint8_t* const dst = a.dst;
+  // a row of zeros; of one that is not finite only the scale says so
+  const bool zeros = !(scale > 0.f && scale < INFINITY);
+  const Quotient q(zeros ? 1.f : scale);
   auto store = [&](int c, const Chunk<S>& v) {
-    *reinterpret_cast<uint2*>(dst + byte_of(r, c, row_bytes, a.tiled)) = scale > 0.f ? quotients(v, q) : uint2{0u, 0u};
+    *reinterpret_cast<uint2*>(a.dst + byte_of(r, c, row_bytes, a.tiled)) = zeros || c >= a.cols ? uint2{0u, 0u} : quotients(v, q);
   };
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i) {
-    const int c = c0 + i * kPass;
-    if (c < a.cols) store(c, held[i]);
-    else if (c < row_bytes) *reinterpret_cast<uint2*>(dst + byte_of(r, c, row_bytes, a.tiled)) = uint2{0u, 0u};
-  }
-  for (int c = c0 + kHeld * kPass; c < row_bytes; c += kPass) {
-    if (c < a.cols) store(c, load_chunk<S, VEC>(row, c, a.cols));
-    else *reinterpret_cast<uint2*>(dst + byte_of(r, c, row_bytes, a.tiled)) = uint2{0u, 0u};
-  }
+  for (int i = 0; i < HELD; ++i)
+    if (c0 + i * kPass < row_bytes) store(c0 + i * kPass, held[i]);
+  for (int c = c0 + HELD * kPass; c < row_bytes; c += kPass) store(c, load_chunk<S, VEC>(row, c, a.cols));
 }
 
-template <typename S, bool VEC> __global__ __launch_bounds__(kThreads) void quantize_kernel(const QuantizeArgs a) {
-  for (int r = blockIdx.x; r < a.rows; r += gridDim.x) {
-    quantize_row<S, VEC>(a, r);
-    __syncthreads();                            // (the maxima are read)
+template <typename S, bool VEC, int LANES, int HELD>
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void quantize_kernel(const QuantizeArgs a) {
+  if constexpr (LANES == 64) {
+    for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < a.rows; r += gridDim.x * 4)
+      quantize_row<S, VEC, 64, HELD>(a, r, threadIdx.x & 63);
+  } else {
+    for (int r = blockIdx.x; r < a.rows; r += gridDim.x) quantize_row<S, VEC, LANES, HELD>(a, r, threadIdx.x);
   }
 }
 
@@ -173,14 +214,23 @@ __global__ __launch_bounds__(kThreads) void pack_i8_kernel(const int8_t* __restr
 
 prism_status launch_quantize(const QuantizeArgs& a, int src_dtype, hipStream_t st) {
   if (a.rows == 0) return PRISM_OK;
-  auto launch = [&](auto elem) {
+  auto launch = [&](auto elem, auto lanes, auto held) {
     using S = decltype(elem);
+    constexpr int kLanes = decltype(lanes)::value, kHeld = decltype(held)::value, kRows = kLanes == 64 ? 4 : 1;
     const bool vec = ((uintptr_t)a.src & 15u) == 0 && a.ld * (long long)sizeof(S) % 16 == 0;
-    if (vec) hipLaunchKernelGGL((quantize_kernel<S, true>), dim3((unsigned)std::min(a.rows, kMaxGrid)), dim3(kThreads), 0, st, a);
-    else hipLaunchKernelGGL((quantize_kernel<S, false>), dim3((unsigned)std::min(a.rows, kMaxGrid)), dim3(kThreads), 0, st, a);
+    const dim3 grid((unsigned)std::min(ceil_div(a.rows, kRows), kMaxGrid)), block(kLanes * kRows);
+    if (vec) hipLaunchKernelGGL((quantize_kernel<S, true, kLanes, kHeld>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((quantize_kernel<S, false, kLanes, kHeld>), grid, block, 0, st, a);
   };
-  if (src_dtype == PRISM_F32) launch(float{});
-  else launch(bf16_t{});
+  // Lanes of a row: enough to hold it, and all there are where rows are too few to fill the machine.
+  auto choose = [&](auto elem) {
+    using std::integral_constant;
+    if (a.cols <= 2048) launch(elem, integral_constant<int, 64>{}, integral_constant<int, 4>{});
+    else if (a.cols <= 8192 && a.rows > 512) launch(elem, integral_constant<int, 256>{}, integral_constant<int, 4>{});
+    else launch(elem, integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+  };
+  if (src_dtype == PRISM_F32) choose(float{});
+  else choose(bf16_t{});
   PRISM_CHECK_LAUNCH();
   return PRISM_OK;
 }
