@@ -18,8 +18,9 @@
 namespace prism {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / 64;
+constexpr int kThreads = 512;           // of balance_kernel
+constexpr int kFinishThreads = 1024;
+constexpr int kBackThreads = 256;
 constexpr int kMaxE = PRISM_MAX_EXPERTS;
 
 struct RowArgs {
@@ -56,6 +57,10 @@ template <int LPR, typename F> __device__ __forceinline__ float over_row(float v
 }
 __device__ __forceinline__ float add(float a, float b) { return a + b; }
 
+// Sets of rows that a wavefront has in flight.
+template <int LPR> constexpr int ahead_of = LPR >= 16 ? 4 : 2;
+template <int LPR> constexpr int back_ahead_of = LPR >= 16 ? 2 : 1;
+
 // The 4 logits of this lane; experts past the last one have -inf.
 __device__ __forceinline__ f32x4 load_row(const RowArgs& a, int row, int e0) {
   const float* p = a.logits + (size_t)row * a.E + e0;
@@ -84,9 +89,10 @@ template <int LPR> __device__ __forceinline__ void softmax_row(f32x4& v) {
 }
 
 // A group's results from its sums: probs, loss and the counts.  sum_p of expert threadIdx.x, in 64 bits; all threads call it.
+template <int THREADS>
 __device__ __forceinline__ void finish_group(int g, int E, int k, int n, int count, double sum_p, int32_t* counts, float* probs,
                                              int32_t* n_tokens, float* loss) {
-  __shared__ double s_term[kThreads];
+  __shared__ double s_term[kMaxE];
   const int e = threadIdx.x;
   double term = 0.0;
   if (e < E) {
@@ -95,8 +101,8 @@ __device__ __forceinline__ void finish_group(int g, int E, int k, int n, int cou
     probs[(size_t)g * E + e] = (float)p;
     term = (double)count * p;
   }
-  s_term[e] = term;
-  for (int half = kThreads / 2; half > 0; half >>= 1) {
+  if (e < kMaxE) s_term[e] = term;
+  for (int half = kMaxE / 2; half > 0; half >>= 1) {
     __syncthreads();
     if (e < half) s_term[e] += s_term[e + half];
   }
@@ -108,21 +114,34 @@ __device__ __forceinline__ void finish_group(int g, int E, int k, int n, int cou
 
 static_assert(kThreads >= kMaxE, "a thread per expert");
 
-// Sums over a part of a group's tokens.  parts == 1: the group's results; else partial sums for finish_kernel: [workgroup]
-// {n, counts [E], probabilities [E]}.  A lane adds the probabilities of its experts over its rows in fp32 (16 of them where
+// Partial sums of `parts` workgroups: probabilities [parts][E4], counts [parts][E4], tokens [parts], with E4 = E rounded up to 4.
+struct Partial {
+  float* probs;
+  int* counts;
+  int* n;
+  int E4;
+};
+__host__ __device__ inline Partial partial_of(void* base, int parts, int E) {
+  const int E4 = (E + 3) / 4 * 4;
+  float* const p = (float*)base;
+  return Partial{p, (int*)p + (size_t)parts * E4, (int*)p + (size_t)parts * E4 * 2, E4};
+}
+
+// Sums over a part of a group's tokens.  parts == 1: the group's results; else partial sums for finish_kernel.  A lane adds the probabilities of its experts over its rows in fp32 (16 of them where
 // 65536 tokens of 256 experts make 1024 parts), the wavefronts' sums are added in their order; the counts are whole
 // numbers, whose order does not matter.
 template <int LPR>
-__global__ __launch_bounds__(kThreads) void balance_kernel(const RowArgs a, int32_t* __restrict__ partial, int32_t* __restrict__ counts,
+__global__ __launch_bounds__(kThreads) void balance_kernel(const RowArgs a, const Partial partial, int32_t* __restrict__ counts,
                                                            float* __restrict__ probs, int32_t* __restrict__ n_tokens,
                                                            float* __restrict__ loss) {
   constexpr int kRows = 64 / LPR;           // rows a wavefront holds
-  constexpr int kAhead = LPR >= 16 ? 4 : 1; // ... and sets of them in flight
+  constexpr int kAhead = ahead_of<LPR>;     // ... and sets of them in flight
+  constexpr int kWaves = kThreads / 64;
   __shared__ int s_counts[kMaxE], s_n;
   __shared__ f32x4 s_sum[kWaves][LPR];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const Rows r = rows_of(a);
-  s_counts[tid] = 0;
+  if (tid < kMaxE) s_counts[tid] = 0;
   if (tid == 0) s_n = 0;
   __syncthreads();
   int live_rows = 0;
@@ -168,51 +187,55 @@ __global__ __launch_bounds__(kThreads) void balance_kernel(const RowArgs a, int3
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) total += s_sum[w][tid / 4][tid % 4];
   if (a.parts == 1) {
-    finish_group(r.group, a.E, a.k, s_n, s_counts[tid], total, counts, probs, n_tokens, loss);
+    finish_group<kThreads>(r.group, a.E, a.k, s_n, tid < kMaxE ? s_counts[tid] : 0, total, counts, probs, n_tokens, loss);
     return;
   }
-  int32_t* out = partial + (size_t)blockIdx.x * (2 * a.E + 1);
-  if (tid == 0) out[0] = s_n;
-  if (tid < a.E) {
-    out[1 + tid] = s_counts[tid];
-    out[1 + a.E + tid] = __float_as_int(total);
+  if (tid == 0) partial.n[blockIdx.x] = s_n;
+  if (tid < partial.E4) {                   // (past E: zeros)
+    partial.counts[(size_t)blockIdx.x * partial.E4 + tid] = s_counts[tid];
+    partial.probs[(size_t)blockIdx.x * partial.E4 + tid] = total;
   }
 }
 
-// The parts of a group, added in 64 bits: thread (slice, expert) the parts slice, slice + slices, ..., then the slices.
-__global__ __launch_bounds__(kThreads) void finish_kernel(const int32_t* __restrict__ partial, int E, int k, int parts,
-                                                          int32_t* __restrict__ counts, float* __restrict__ probs,
-                                                          int32_t* __restrict__ n_tokens, float* __restrict__ loss) {
-  __shared__ double s_sum[kThreads];
-  __shared__ int s_count[kThreads], s_n[kThreads];
+// The parts of a group, added in 64 bits: thread (slice, 4 experts) the parts slice, slice + slices, ..., then pairs of slices.
+__global__ __launch_bounds__(kFinishThreads) void finish_kernel(const Partial partial, int E, int k, int parts, int lanes,
+                                                                int32_t* __restrict__ counts, float* __restrict__ probs,
+                                                                int32_t* __restrict__ n_tokens, float* __restrict__ loss) {
+  __shared__ double s_sum[kFinishThreads][4];
+  __shared__ int s_count[kFinishThreads][4], s_n[kFinishThreads];
   const int tid = threadIdx.x, g = blockIdx.x;
-  const int slices = kThreads / E;          // (1 to 256 experts)
-  const int slice = tid / E, e = tid - slice * E;
-  const int32_t* group = partial + (size_t)g * parts * (2 * E + 1);
-  double sum = 0.0;
-  int count = 0, n = 0;
-  if (slice < slices)
-#pragma unroll 4
+  const int slices = kFinishThreads / lanes, slice = tid / lanes, e0 = tid % lanes * 4;
+  double sum[4] = {0., 0., 0., 0.};
+  int count[4] = {0, 0, 0, 0}, n = 0;
+  if (e0 < E)
+#pragma unroll 8
     for (int p = slice; p < parts; p += slices) {
-      const int32_t* in = group + (size_t)p * (2 * E + 1);
-      n += in[0];
-      count += in[1 + e];
-      sum += (double)__int_as_float(in[1 + E + e]);
+      const size_t at = (size_t)g * parts + p;
+      n += partial.n[at];
+      const int4 c = *reinterpret_cast<const int4*>(partial.counts + at * partial.E4 + e0);
+      const f32x4 v = *reinterpret_cast<const f32x4*>(partial.probs + at * partial.E4 + e0);
+      count[0] += c.x; count[1] += c.y; count[2] += c.z; count[3] += c.w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum[i] += (double)v[i];
     }
-  s_sum[tid] = sum;
-  s_count[tid] = count;
-  s_n[tid] = n;
-  __syncthreads();
-  sum = 0.0;
-  count = n = 0;
-  for (int s = 0; s < slices; ++s) {
-    n += s_n[s * E];
-    if (tid < E) {
-      count += s_count[s * E + tid];
-      sum += s_sum[s * E + tid];
+  for (int half = slices; half > 0; half >>= 1) {   // the first round only writes
+    if (slice < half) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (half < slices) {
+          sum[i] += s_sum[tid + half * lanes][i];
+          count[i] += s_count[tid + half * lanes][i];
+        }
+        s_sum[tid][i] = sum[i];
+        s_count[tid][i] = count[i];
+      }
+      if (half < slices) n += s_n[tid + half * lanes];
+      s_n[tid] = n;
     }
+    __syncthreads();
   }
-  finish_group(g, E, k, n, count, sum, counts, probs, n_tokens, loss);
+  finish_group<kFinishThreads>(g, E, k, s_n[0], tid < E ? s_count[tid / 4][tid % 4] : 0, tid < E ? s_sum[tid / 4][tid % 4] : 0.0,
+                               counts, probs, n_tokens, loss);
 }
 
 struct BackwardArgs {
@@ -225,13 +248,21 @@ struct BackwardArgs {
   int softmax_all;
 };
 
-// Slot j of a row's picks belongs to lane j % LPR of the row, register j / LPR.
+// Slot j of a row's picks belongs to lane j % LPR of the row, register j / LPR; in rows of 16 lanes and more every 16 of them
+// hold all slots (a lane's value then reaches the 16 by one move inside the vector ALU, row_newbcast).
 template <int LPR> constexpr int slots_of = LPR >= PRISM_MAX_TOPK ? 1 : PRISM_MAX_TOPK / LPR;
+template <int LPR> constexpr int slot_lanes_of = LPR > 16 ? 16 : LPR;
+template <int LPR, int J> __device__ __forceinline__ int slot_value(const int (&v)[slots_of<LPR>]) {
+  const int x = v[J / LPR];
+  if constexpr (LPR == 1) return x;
+  else if constexpr (LPR >= 16) return dpp_move<0x150 + J>(x, x);
+  else return __shfl(x, J % LPR, LPR);
+}
 
 template <int LPR>
-__global__ __launch_bounds__(kThreads) void route_backward_kernel(const BackwardArgs b) {
-  constexpr int kRows = 64 / LPR, SL = slots_of<LPR>;
-  constexpr int kAhead = LPR >= 16 ? 2 : 1;
+__global__ __launch_bounds__(kBackThreads) void route_backward_kernel(const BackwardArgs b) {
+  constexpr int kRows = 64 / LPR, SL = slots_of<LPR>, kSlotLanes = slot_lanes_of<LPR>;
+  constexpr int kAhead = back_ahead_of<LPR>, kWaves = kBackThreads / 64;
   const RowArgs& a = b.r;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int in_row = lane % LPR, e0 = in_row * 4;
@@ -262,7 +293,7 @@ __global__ __launch_bounds__(kThreads) void route_backward_kernel(const Backward
       v[s] = load_row(a, row, e0);
 #pragma unroll
       for (int q = 0; q < SL; ++q) {
-        const int j = in_row + q * LPR;
+        const int j = in_row % kSlotLanes + q * LPR;
         idx[s][q] = -1;
         dg[s][q] = 0.f;
         if (b.d_gate != nullptr && j < a.k) {
@@ -282,7 +313,7 @@ __global__ __launch_bounds__(kThreads) void route_backward_kernel(const Backward
         float m = -INFINITY;
 #pragma unroll
         for (int q = 0; q < SL; ++q) m = fmaxf(m, l[s][q]);
-        m = over_row<LPR>(m, [](float x, float y) { return fmaxf(x, y); });
+        m = over_row<kSlotLanes>(m, [](float x, float y) { return fmaxf(x, y); });
         if (m == -INFINITY) m = 0.f;
         float sum = 0.f, dot = 0.f;
 #pragma unroll
@@ -291,8 +322,8 @@ __global__ __launch_bounds__(kThreads) void route_backward_kernel(const Backward
           sum += t[q];
           dot += t[q] * dg[s][q];
         }
-        sum = over_row<LPR>(sum, add);
-        dot = over_row<LPR>(dot, add);
+        sum = over_row<kSlotLanes>(sum, add);
+        dot = over_row<kSlotLanes>(dot, add);
         const float inv = sum > 0.f ? 1.0f / sum : sum;
 #pragma unroll
         for (int q = 0; q < SL; ++q) t[q] = t[q] * inv * (dg[s][q] - dot * inv);
@@ -301,19 +332,27 @@ __global__ __launch_bounds__(kThreads) void route_backward_kernel(const Backward
         for (int q = 0; q < SL; ++q) t[q] = dg[s][q];
       }
       f32x4 g = {0.f, 0.f, 0.f, 0.f};       // of this lane's experts
-      if (b.d_gate != nullptr)
+      if (b.d_gate != nullptr) {
+        int bits[SL];
 #pragma unroll
-        for (int j = 0; j < PRISM_MAX_TOPK; ++j) {
-          if (j >= a.k) break;
-          int e = idx[s][j / LPR];
-          float x = t[j / LPR];
-          if constexpr (LPR > 1) {
-            e = __shfl(e, j % LPR, LPR);
-            x = __shfl(x, j % LPR, LPR);
-          }
+        for (int q = 0; q < SL; ++q) bits[q] = __float_as_int(t[q]);
+        auto add_slot = [&](auto j) {
+          if (j.value >= a.k) return;
+          const int d = slot_value<LPR, j.value>(idx[s]) - e0;
+          const float x = __int_as_float(slot_value<LPR, j.value>(bits));
 #pragma unroll
-          for (int i = 0; i < 4; ++i) g[i] += e == e0 + i ? x : 0.f;
-        }
+          for (int i = 0; i < 4; ++i) g[i] += d == i ? x : 0.f;
+        };
+        add_slot(std::integral_constant<int, 0>{});
+        add_slot(std::integral_constant<int, 1>{});
+        add_slot(std::integral_constant<int, 2>{});
+        add_slot(std::integral_constant<int, 3>{});
+        add_slot(std::integral_constant<int, 4>{});
+        add_slot(std::integral_constant<int, 5>{});
+        add_slot(std::integral_constant<int, 6>{});
+        add_slot(std::integral_constant<int, 7>{});
+        static_assert(PRISM_MAX_TOPK == 8, "all slots");
+      }
       f32x4 w = u;
       if (b.softmax_all) w += g;
       const float mean = over_row<LPR>((w[0] * v[s][0] + w[1] * v[s][1]) + (w[2] * v[s][2] + w[3] * v[s][3]), add);
@@ -350,20 +389,17 @@ template <typename Fn> void with_lanes(int E, Fn&& fn) {
   else fn(std::integral_constant<int, 64>{});
 }
 
-constexpr int kBlocks = 1024;     // workgroups that a batch is cut into, about
-constexpr int kMaxGroups = PRISM_MAX_BALANCE_GROUPS;   // (a workgroup each: below 2^31 threads)
-constexpr int kFewRows = 16;      // rows per lane group and wavefront, at least
+constexpr int kParts = 512;       // workgroups that share the tokens of a batch in balance_kernel, about
+constexpr int kBackParts = 2048;  // ... and in route_backward_kernel, which leaves no sums to be added
+constexpr int kMaxGroups = PRISM_MAX_BALANCE_GROUPS;   // (a workgroup each: below 2^32 threads)
 
-// The groups of a batch, and how many workgroups share one.
-int split_groups(RowArgs* a, int group_tokens, int T, int max_parts_total) {
+// The groups of a batch, and how many workgroups share one: at least one pass of rows each.
+int split_groups(RowArgs* a, int group_tokens, int T, int most, int rows_per_pass) {
   a->group = group_tokens > 0 ? group_tokens : std::max(T, 1);
   const int G = group_tokens > 0 ? (int)(((long long)T + group_tokens - 1) / group_tokens) : 1;
-  int lanes = 1;
-  while (lanes * 4 < a->E) lanes *= 2;
-  const int rows_per_pass = kWaves * (64 / lanes);
   const int rows = std::min(a->group, std::max(T, 1));
-  const int wanted = std::max(1, max_parts_total / std::max(G, 1));
-  a->part_rows = std::max(ceil_div(rows, wanted), rows_per_pass * kFewRows);
+  const int wanted = std::max(1, most / std::max(G, 1));
+  a->part_rows = std::max(ceil_div(rows, wanted), rows_per_pass);
   a->parts = ceil_div(rows, a->part_rows);
   return G;
 }
@@ -372,25 +408,30 @@ bool aligned16(const void* a, const void* b) { return (((uintptr_t)a | (uintptr_
 
 }  // namespace
 
-size_t balance_workspace_bytes(int E) { return align_up((size_t)kBlocks * (2 * E + 1) * 4, 256); }
+size_t balance_workspace_bytes(int E) { return align_up((size_t)kParts * (2 * align_up(E, 4) + 1) * 4, 256); }
 
 prism_status launch_balance(const prism_layer_desc& d, const float* logits, const int32_t* topk_idx, const uint8_t* mask,
                             int group_tokens, int T, float* loss, int32_t* counts, float* probs, int32_t* n_tokens,
                             void* workspace, hipStream_t st) {
+  if (T == 0 && group_tokens > 0) return PRISM_OK;    // no groups
   RowArgs a{logits, topk_idx, mask, T, d.n_experts, d.top_k, 0, 1, 0, d.n_experts % 4 == 0 && aligned16(logits, nullptr)};
-  const int G = split_groups(&a, group_tokens, T, kBlocks);
-  if (G == 0) return PRISM_OK;
-  if (G > kMaxGroups) return PRISM_ERR_UNSUPPORTED;
+  prism_status status = PRISM_OK;
   with_lanes(a.E, [&](auto lanes) {
-    hipLaunchKernelGGL((balance_kernel<lanes.value>), dim3((unsigned)G * a.parts), dim3(kThreads), 0, st, a, (int32_t*)workspace,
-                       counts, probs, n_tokens, loss);
+    constexpr int LPR = decltype(lanes)::value;
+    const int G = split_groups(&a, group_tokens, T, kParts, kThreads / LPR * ahead_of<LPR>);
+    if (G > kMaxGroups) {
+      status = PRISM_ERR_UNSUPPORTED;
+      return;
+    }
+    const Partial partial = partial_of(workspace, G * a.parts, a.E);
+    hipLaunchKernelGGL((balance_kernel<LPR>), dim3((unsigned)G * a.parts), dim3(kThreads), 0, st, a, partial, counts, probs, n_tokens,
+                       loss);
+    if (a.parts > 1)
+      hipLaunchKernelGGL(finish_kernel, dim3((unsigned)G), dim3(kFinishThreads), 0, st, partial, a.E, a.k, a.parts, LPR, counts, probs,
+                         n_tokens, loss);
   });
+  PRISM_TRY(status);
   PRISM_CHECK_LAUNCH();
-  if (a.parts > 1) {
-    hipLaunchKernelGGL(finish_kernel, dim3((unsigned)G), dim3(kThreads), 0, st, (const int32_t*)workspace, a.E, a.k, a.parts,
-                       counts, probs, n_tokens, loss);
-    PRISM_CHECK_LAUNCH();
-  }
   return PRISM_OK;
 }
 
@@ -400,11 +441,17 @@ prism_status launch_route_backward(const prism_layer_desc& d, const float* logit
   if (T == 0) return PRISM_OK;
   BackwardArgs b{{logits, topk_idx, mask, T, d.n_experts, d.top_k, 0, 1, 0, d.n_experts % 4 == 0 && aligned16(logits, d_logits)},
                  d_gate, counts, n_tokens, d_loss, d_logits, d.gate_mode == PRISM_GATES_SOFTMAX_ALL};
-  const int G = split_groups(&b.r, counts != nullptr ? group_tokens : 0, T, 2 * kBlocks);
-  if (G > kMaxGroups) return PRISM_ERR_UNSUPPORTED;
+  prism_status status = PRISM_OK;
   with_lanes(b.r.E, [&](auto lanes) {
-    hipLaunchKernelGGL((route_backward_kernel<lanes.value>), dim3((unsigned)G * b.r.parts), dim3(kThreads), 0, st, b);
+    constexpr int LPR = decltype(lanes)::value;
+    const int G = split_groups(&b.r, counts != nullptr ? group_tokens : 0, T, kBackParts, kBackThreads / LPR * back_ahead_of<LPR>);
+    if (G > kMaxGroups) {
+      status = PRISM_ERR_UNSUPPORTED;
+      return;
+    }
+    hipLaunchKernelGGL((route_backward_kernel<LPR>), dim3((unsigned)G * b.r.parts), dim3(kBackThreads), 0, st, b);
   });
+  PRISM_TRY(status);
   PRISM_CHECK_LAUNCH();
   return PRISM_OK;
 }
