@@ -117,8 +117,9 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 
 def _stream(stream: Optional[torch.cuda.Stream]) -> Optional[int]:
-    s = torch.cuda.current_stream() if stream is None else stream
-    return s.cuda_stream or None
+    # (the stream object of the current device's stream takes 2.5 us to make)
+    s = torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) if stream is None else stream.cuda_stream
+    return s or None
 
 
 def make_desc(hidden: int, ffn: int, n_experts: int, top_k: int, n_shared: int = 0,
@@ -194,15 +195,17 @@ def alloc_balance_workspace(desc: LayerDesc, device="cuda") -> torch.Tensor:
     return torch.empty(n.value, dtype=torch.uint8, device=device)
 
 
-def _typed(t: Optional[torch.Tensor], dtype: torch.dtype, shape, what: str) -> Optional[int]:
+def _typed(t: Optional[torch.Tensor], dtype: torch.dtype, shape: tuple, what: str) -> Optional[int]:
     """The address of a tensor that has to be of this type and shape, on the device the call is enqueued on."""
     if t is None:
         return None
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
-        raise PrismError(f"{what} has to be {dtype} {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
-    if t.device.index != torch.cuda.current_device():
+    if t.dtype != dtype or t.shape != shape:
+        raise PrismError(f"{what} has to be {dtype} {shape}, not {t.dtype} {tuple(t.shape)}")
+    if t.get_device() != torch.cuda.current_device():
         raise PrismError(f"{what} is on {t.device}, not on the current device")
-    return _ptr(t)
+    if not t.is_contiguous():
+        raise PrismError(f"{what} has to be contiguous")
+    return t.data_ptr()
 
 
 @dataclass
@@ -223,12 +226,12 @@ def prism_balance_loss(desc: LayerDesc, logits, topk_idx, workspace, token_mask=
 
     logits [T, E] and topk_idx [T, k] as prism_route returns them; token_mask [T] uint8, 0 for padding."""
     T, E, k = logits.shape[0], desc.n_experts, desc.top_k
-    G, dev = _balance_groups(T, group_tokens), logits.device
+    G = _balance_groups(T, group_tokens)
     f32, i32 = torch.float32, torch.int32
     o = outputs
     if o is None:
-        o = BalanceOut(torch.empty((G,), dtype=f32, device=dev), torch.empty((G, E), dtype=i32, device=dev),
-                       torch.empty((G, E), dtype=f32, device=dev), torch.empty((G,), dtype=i32, device=dev))
+        new = logits.new_empty
+        o = BalanceOut(new((G,), dtype=f32), new((G, E), dtype=i32), new((G, E), dtype=f32), new((G,), dtype=i32))
     if G == 0:                  # no tokens, no groups: nothing to address
         return o
     _check(load_library().prism_balance_loss(
@@ -250,7 +253,7 @@ def prism_route_backward(desc: LayerDesc, logits, topk_idx, balance: Optional[Ba
     if (balance is None) != (d_loss is None):
         raise PrismError("d_loss comes with the balance it is the gradient of")
     if d_logits is None:
-        d_logits = torch.empty((T, E), dtype=f32, device=logits.device)
+        d_logits = logits.new_empty((T, E), dtype=f32)
     if T == 0:
         return d_logits
     _check(load_library().prism_route_backward(
@@ -496,28 +499,32 @@ class I8Matrix:
                 self.data[R * C:R * C + 4 * self.rows].clone().view(torch.float32))
 
 
-def _alloc_i8(rows: int, cols: int, device) -> torch.Tensor:
-    n = ctypes.c_size_t(0)
-    if rows > 0:
-        _check(load_library().prism_i8_bytes(rows, cols, ctypes.byref(n)), "prism_i8_bytes")
-    return torch.empty(n.value, dtype=torch.uint8, device=device)
+def _i8_bytes(rows: int, cols: int) -> int:
+    """prism_i8_bytes, for sizes that the call the buffer is for will check."""
+    R = -(-rows // 16) * 16
+    return -(-(R * (-(-cols // 128) * 128) + 4 * R) // 256) * 256
 
 
 def _rows_ptr(t: torch.Tensor, dtypes, what: str):
     """(address, elements from row to row) of a matrix whose rows are contiguous."""
-    if t.dim() != 2 or t.dtype not in dtypes or not t.is_cuda:
+    if t.dim() != 2 or t.dtype not in dtypes:
         raise PrismError(f"{what} has to be a device matrix of {' or '.join(map(str, dtypes))}")
-    if t.device.index != torch.cuda.current_device():
+    if t.get_device() != torch.cuda.current_device():
         raise PrismError(f"{what} is on {t.device}, not on the current device")
     rows, cols = t.shape
-    if cols > 1 and t.stride(1) != 1 or rows > 1 and t.stride(0) < cols:
-        raise PrismError(f"{what} has to have contiguous rows that do not overlap")
-    return t.data_ptr(), t.stride(0) if rows > 1 else cols
+    ld = cols
+    if not t.is_contiguous():
+        ld, step = t.stride()
+        if rows <= 1:
+            ld = cols
+        if cols > 1 and step != 1 or ld < cols:
+            raise PrismError(f"{what} has to have contiguous rows that do not overlap")
+    return t.data_ptr(), ld
 
 
-def _out_i8(out: Optional[I8Matrix], rows: int, cols: int, device) -> I8Matrix:
+def _out_i8(out: Optional[I8Matrix], rows: int, cols: int, like: torch.Tensor) -> I8Matrix:
     if out is None:
-        return I8Matrix(_alloc_i8(rows, cols, device), rows, cols)
+        return I8Matrix(like.new_empty((_i8_bytes(rows, cols),), dtype=torch.uint8), rows, cols)
     if (out.rows, out.cols) != (rows, cols):
         raise PrismError(f"out is an 8-bit matrix of {out.rows} x {out.cols}, not {rows} x {cols}")
     return out
@@ -527,7 +534,7 @@ def prism_quantize_i8(src, out: Optional[I8Matrix] = None, stream=None) -> I8Mat
     """fp32 or bf16 rows -> 8 bits with a scale per row (see prism.h)."""
     ptr, ld = _rows_ptr(src, (torch.float32, torch.bfloat16), "src")
     rows, cols = src.shape
-    o = _out_i8(out, rows, cols, src.device)
+    o = _out_i8(out, rows, cols, src)
     _check(load_library().prism_quantize_i8(ptr, PRISM_F32 if src.dtype == torch.float32 else PRISM_BF16, ld, rows, cols,
                                             _ptr(o.data), _stream(stream)), "prism_quantize_i8")
     return o
@@ -537,7 +544,7 @@ def prism_pack_i8(q, scale, out: Optional[I8Matrix] = None, stream=None) -> I8Ma
     """int8 rows and their fp32 scales, as a checkpoint holds them -> the library's layout."""
     ptr, ld = _rows_ptr(q, (torch.int8,), "q")
     rows, cols = q.shape
-    o = _out_i8(out, rows, cols, q.device)
+    o = _out_i8(out, rows, cols, q)
     _check(load_library().prism_pack_i8(ptr, ld, _typed(scale, torch.float32, (rows,), "scale"), rows, cols, _ptr(o.data),
                                         _stream(stream)), "prism_pack_i8")
     return o
@@ -554,8 +561,8 @@ def prism_matmul_i8(a: I8Matrix, b: I8Matrix, workspace, out=None, dtype=torch.b
     if a.cols != b.cols:
         raise PrismError(f"rows of {a.cols} and of {b.cols} elements")
     if out is None:
-        out = torch.empty((a.rows, b.rows), dtype=dtype, device=b.data.device)
-    if tuple(out.shape) != (a.rows, b.rows):
+        out = b.data.new_empty((a.rows, b.rows), dtype=dtype)
+    elif out.shape != (a.rows, b.rows):
         raise PrismError(f"out has to be {a.rows} x {b.rows}, not {tuple(out.shape)}")
     ptr, ldo = _rows_ptr(out, (torch.float32, torch.bfloat16), "out")
     _check(load_library().prism_matmul_i8(_ptr(a.data), _ptr(b.data), a.rows, b.rows, a.cols, ptr, ldo,

@@ -51,10 +51,16 @@ template <int LPR, typename F> __device__ __forceinline__ float over_row(float v
   if constexpr (LPR > 2) v = f(v, row_xor<2>(v));
   if constexpr (LPR > 4) v = f(v, row_xor<4>(v));
   if constexpr (LPR > 8) v = f(v, row_xor<8>(v));
-  if constexpr (LPR > 16) v = f(v, __shfl_xor(v, 16));
-  if constexpr (LPR > 32) v = f(v, __shfl_xor(v, 32));
+  if constexpr (LPR == 32) v = f(v, __shfl_xor(v, 16));
+  if constexpr (LPR == 64) {                    // (the row is the wavefront: its four parts through scalar registers)
+    auto part = [&](int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); };
+    v = f(f(part(0), part(16)), f(part(32), part(48)));
+  }
   return v;
 }
+
+// e^x for x <= 0 by the hardware's exp2, which is within 1 ulp: the product with log2 e is off by |x| 2^-24 of the result's value.
+__device__ __forceinline__ float exp_neg(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
 __device__ __forceinline__ float add(float a, float b) { return a + b; }
 
 // Sets of rows that a wavefront has in flight.
@@ -81,7 +87,7 @@ template <int LPR> __device__ __forceinline__ void softmax_row(f32x4& v) {
   float m = over_row<LPR>(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), [](float x, float y) { return fmaxf(x, y); });
   if (m == -INFINITY) m = 0.f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = expf(v[i] - m);
+  for (int i = 0; i < 4; ++i) v[i] = exp_neg(v[i] - m);
   const float s = over_row<LPR>((v[0] + v[1]) + (v[2] + v[3]), add);
   const float inv = s > 0.f ? 1.0f / s : s;     // (a NaN stays one)
 #pragma unroll
@@ -318,7 +324,7 @@ __global__ __launch_bounds__(kBackThreads) void route_backward_kernel(const Back
         float sum = 0.f, dot = 0.f;
 #pragma unroll
         for (int q = 0; q < SL; ++q) {
-          t[q] = expf(l[s][q] - m);
+          t[q] = exp_neg(l[s][q] - m);
           sum += t[q];
           dot += t[q] * dg[s][q];
         }
@@ -393,13 +399,15 @@ constexpr int kParts = 512;       // workgroups that share the tokens of a batch
 constexpr int kBackParts = 2048;  // ... and in route_backward_kernel, which leaves no sums to be added
 constexpr int kMaxGroups = PRISM_MAX_BALANCE_GROUPS;   // (a workgroup each: below 2^32 threads)
 
-// The groups of a batch, and how many workgroups share one: at least one pass of rows each.
-int split_groups(RowArgs* a, int group_tokens, int T, int most, int rows_per_pass) {
+// The groups of a batch, and how many workgroups share one: at least one pass of rows each, and one workgroup for up to
+// `few` passes (another pass takes less than the launch that adds the parts).
+int split_groups(RowArgs* a, int group_tokens, int T, int most, int rows_per_pass, int few) {
   a->group = group_tokens > 0 ? group_tokens : std::max(T, 1);
   const int G = group_tokens > 0 ? (int)(((long long)T + group_tokens - 1) / group_tokens) : 1;
   const int rows = std::min(a->group, std::max(T, 1));
   const int wanted = std::max(1, most / std::max(G, 1));
   a->part_rows = std::max(ceil_div(rows, wanted), rows_per_pass);
+  if (rows <= few * rows_per_pass) a->part_rows = rows;
   a->parts = ceil_div(rows, a->part_rows);
   return G;
 }
@@ -418,7 +426,7 @@ prism_status launch_balance(const prism_layer_desc& d, const float* logits, cons
   prism_status status = PRISM_OK;
   with_lanes(a.E, [&](auto lanes) {
     constexpr int LPR = decltype(lanes)::value;
-    const int G = split_groups(&a, group_tokens, T, kParts, kThreads / LPR * ahead_of<LPR>);
+    const int G = split_groups(&a, group_tokens, T, kParts, kThreads / LPR * ahead_of<LPR>, 4);
     if (G > kMaxGroups) {
       status = PRISM_ERR_UNSUPPORTED;
       return;
@@ -444,7 +452,7 @@ prism_status launch_route_backward(const prism_layer_desc& d, const float* logit
   prism_status status = PRISM_OK;
   with_lanes(b.r.E, [&](auto lanes) {
     constexpr int LPR = decltype(lanes)::value;
-    const int G = split_groups(&b.r, counts != nullptr ? group_tokens : 0, T, kBackParts, kBackThreads / LPR * back_ahead_of<LPR>);
+    const int G = split_groups(&b.r, counts != nullptr ? group_tokens : 0, T, kBackParts, kBackThreads / LPR * back_ahead_of<LPR>, 1);
     if (G > kMaxGroups) {
       status = PRISM_ERR_UNSUPPORTED;
       return;

@@ -222,10 +222,11 @@ prism_status launch_quantize(const QuantizeArgs& a, int src_dtype, hipStream_t s
     if (vec) hipLaunchKernelGGL((quantize_kernel<S, true, kLanes, kHeld>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((quantize_kernel<S, false, kLanes, kHeld>), grid, block, 0, st, a);
   };
-  // Lanes of a row: enough to hold it, and all there are where rows are too few to fill the machine.
+  // Lanes of a row: a wavefront where rows are many and it holds them; else as many as make one or two passes of it.
   auto choose = [&](auto elem) {
     using std::integral_constant;
-    if (a.cols <= 2048) launch(elem, integral_constant<int, 64>{}, integral_constant<int, 4>{});
+    if (a.cols <= 2048 && a.rows > 4096) launch(elem, integral_constant<int, 64>{}, integral_constant<int, 4>{});
+    else if (a.cols <= 2048) launch(elem, integral_constant<int, 256>{}, integral_constant<int, 1>{});
     else if (a.cols <= 8192 && a.rows > 512) launch(elem, integral_constant<int, 256>{}, integral_constant<int, 4>{});
     else launch(elem, integral_constant<int, 1024>{}, integral_constant<int, 2>{});
   };

@@ -17,6 +17,8 @@ def _bytes(rows, cols):
 @pytest.mark.parametrize("rows,cols,elements", [(1, 1, 16 * 128), (16, 128, 16 * 128), (17, 129, 32 * 256), (14336, 4096, 14336 * 4096)])
 def test_size(rows, cols, elements):
     status, n = _bytes(rows, cols)
+    from paper_2508_12851_amd import binding
+    assert binding._i8_bytes(rows, cols) == n
     assert status == 0 and n == -(-(elements + 4 * (-(-rows // 16) * 16)) // 256) * 256
 
 
