@@ -109,7 +109,7 @@ prism_status run_i8_ffn(const prism_layer_desc& d, const void* x, const prism_ex
   else
     PRISM_TRY((gg::launch_gemm<C2::BM, C2::BN, 2, 2, C2::BK, C2::STAGES, false, SPLIT_DOWN, ROTATE, STREAM_B, false, true>(
         g2, capacity2, st)));
-  if constexpr (kPrefill) {
+  if constexpr (kPrefill && C2::STAGES == 4) {   // (layers whose last round may be cut have long contractions)
     if (f.slice_kt2 > 0) {   // the cut last round: one slice entry per workgroup, fp32 partial tiles
       PRISM_TRY((gg::launch_gemm<C2::BM, C2::BN, 2, 2, C2::BK, C2::STAGES, false, false, false, false, true, true>(
           g2, capacity2, st)));

@@ -82,7 +82,7 @@ struct GemmArgs {
   void* dense_out;          // [c_rows, N] with dense_ldo elements from row to row
   long long dense_ldo;
   int dense_f32;            // fp32 instead of bf16
-  int dense_vec;            // rows can be stored 4 elements at a time
+  int dense_vec;            // 1: rows can be stored 4 elements at a time; 2: bf16, 8 elements
   int dense_splits;         // SPLITK: workgroups that share an item
 };
 
@@ -137,6 +137,26 @@ template <int WM, int WN, bool GATED> struct ScaleSlot {
   static constexpr int kBytes = (kRowLoads + (GATED ? 2 : 1) * kColLoads) * 256;
 };
 
+// LDS of one workgroup of a tile shape, and how many of them a CU holds.  (Four wavefronts, WGN of them side by side.)
+constexpr int kLdsBytes = 160 * 1024;
+template <int BM, int BN, int WGN, int BK, int STAGES, bool GATED, bool I8>
+constexpr int gemm_lds_unstaged() {
+  return STAGES * (BM + BN) * BK * 2 + (GATED ? 4096 : 0) +           // ring + source-row slots
+         (I8 ? 4 * 2 * ScaleSlot<BM * WGN / 4, BN / WGN, GATED>::kBytes : 0);
+}
+// 8-bit products go through the strips where there is room for them (h, as above, does not: gate/up of 4096 tokens of the
+// 4096 x 14336 layer 803 us against 821 through strips of 32 fp32 columns; the product of 8192 x 8192 x 4096 275 -> 228 us).
+template <int BM, int BN, int WGN, int BK, int STAGES, bool GATED, bool SPLITK, bool SLICES>
+constexpr bool staged_store_i8() {
+  return !SPLITK && !SLICES && !GATED && (BN / WGN / 32) % 2 == 0 &&
+         gemm_lds_unstaged<BM, BN, WGN, BK, STAGES, GATED, true>() + 4 * kStripBytes <= kLdsBytes;
+}
+template <int BM, int BN, int WGN, int BK, int STAGES, bool GATED, bool SPLITK, bool I8 = false, bool SLICES = false>
+constexpr int gemm_lds_bytes() {
+  constexpr bool staged = I8 ? staged_store_i8<BM, BN, WGN, BK, STAGES, GATED, SPLITK, SLICES>()
+                             : staged_store<BN / WGN, GATED, SPLITK>();
+  return gemm_lds_unstaged<BM, BN, WGN, BK, STAGES, GATED, I8>() + (staged ? 4 * kStripBytes : 0);   // + strips
+}
 // Elements n .. n + 3 of a row of a dense product with N columns.
 __device__ __forceinline__ void store_dense(void* out, long long ldo, int f32, int vec, size_t row, int n, int N, const f32x4& v) {
   if (f32) {
@@ -228,17 +248,10 @@ static inline prism_status launch_build_schedules(const prism_layer_desc& d,
   return PRISM_OK;
 }
 
-// LDS of one workgroup of a tile shape, and how many of them a CU holds.
-// (Four wavefronts, WGN of them side by side.)
-template <int BM, int BN, int WGN, int BK, int STAGES, bool GATED, bool SPLITK, bool I8 = false>
-constexpr int gemm_lds_bytes() {
-  return (I8 ? 4 * 2 * ScaleSlot<BM * WGN / 4, BN / WGN, GATED>::kBytes : 0) + STAGES * (BM + BN) * BK * 2 + (GATED ? 4096 : 0) +           // ring + source-row slots
-         (!I8 && staged_store<BN / WGN, GATED, SPLITK>() ? 4 * kStripBytes : 0);   // + strips
-}
 constexpr int kCusPerXcd = 32;
 template <int BM, int BN, int WGN, int BK, int STAGES, bool GATED, bool SPLITK, bool I8 = false>
 constexpr int gemm_wgs_per_xcd() {
-  return kCusPerXcd * ((160 * 1024) / gemm_lds_bytes<BM, BN, WGN, BK, STAGES, GATED, SPLITK, I8>());
+  return kCusPerXcd * (kLdsBytes / gemm_lds_bytes<BM, BN, WGN, BK, STAGES, GATED, SPLITK, I8>());
 }
 
 // capacity: items per XCD list (sched_capacity).  The grid holds as many workgroups
@@ -246,7 +259,7 @@ constexpr int gemm_wgs_per_xcd() {
 template <int BM, int BN, int WGM, int WGN, int BK, int STAGES, bool GATED, bool SPLITK = false,
           bool ROTATE = false, bool STREAM_B = false, bool SLICES = false, bool I8 = false, bool DENSE = false>
 prism_status launch_gemm(const GemmArgs& args, int capacity, hipStream_t st, int max_slots = 0) {
-  constexpr int smem = gemm_lds_bytes<BM, BN, WGN, BK, STAGES, GATED, SPLITK, I8>();
+  constexpr int smem = gemm_lds_bytes<BM, BN, WGN, BK, STAGES, GATED, SPLITK, I8, SLICES>();
   static_assert(smem <= 160 * 1024, "LDS per workgroup");
   auto kernel = grouped_gemm_kernel<BM, BN, WGM, WGN, BK, STAGES, GATED, SPLITK, ROTATE, STREAM_B, SLICES, I8, DENSE>;
   static LdsLimitOnce lds_limit;   // one per instantiation

@@ -24,7 +24,8 @@
   static_assert((STAGES - 1) * LPS <= 63, "vmcnt is a 6-bit counter");
 
   // wide bf16 output tiles are stored through LDS strips (see the epilogue)
-  constexpr bool kStagedStore = !I8 && staged_store<WN, GATED, SPLITK>();
+  constexpr bool kStagedStore = I8 ? staged_store_i8<BM, BN, WGN, BK, STAGES, GATED, SPLITK, SLICES>()
+                                   : staged_store<WN, GATED, SPLITK>();
   constexpr int kStripBase = STAGES * kStageBytes + (GATED ? 4096 : 0);
   constexpr int kScaleBase = kStripBase + (kStagedStore ? 4 * kStripBytes : 0);   // I8: see "scales" below
 
@@ -462,31 +463,47 @@
       for (int w8 = 0; w8 < 8; ++w8) cur[w8] = nxt[w8];
     }
   };
+  // The scales of 32 columns of the wavefront from float `at` on as this lane takes them (register quad vg: columns 8 vg + 4 q ..),
+  // and of a row.  From assembly, as in epilogue_staged: before an LDS access that the compiler sees it waits for every direct-to-LDS load
+  // in flight, and with them for every store.
+  const uint32_t scale_lds = (uint32_t)(uintptr_t)(lds_ptr_t)(smem + scale_slot);
+  auto read_cols = [&](int parity, int at, f32x4 (&c)[4]) {
+    const uint32_t a = scale_lds + (uint32_t)(parity * Slot::kBytes + (Slot::kRowLoads * 64 + at) * 4 + q * 16);
+    f32x4 c0, c1, c2, c3;
+    asm volatile(
+        "ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:32\n\tds_read_b128 %2, %4 offset:64\n\t"
+        "ds_read_b128 %3, %4 offset:96\n\ts_waitcnt lgkmcnt(0)"
+        : "=&v"(c0), "=&v"(c1), "=&v"(c2), "=&v"(c3) : "v"(a) : "memory");
+    c[0] = c0; c[1] = c1; c[2] = c2; c[3] = c3;
+  };
+  auto read_row_scales = [&](int parity, float (&rs)[MI]) {
+    const uint32_t a = scale_lds + (uint32_t)(parity * Slot::kBytes + r32 * 4);
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+      asm volatile("ds_read_b32 %0, %1 offset:%2\n\ts_waitcnt lgkmcnt(0)" : "=&v"(rs[i]) : "v"(a), "n"(i * 128) : "memory");
+  };
+
   // I8: sums of whole numbers times the scales of their row and column.
   auto epilogue_i8 = [&](const Ctx& cx, int parity) {
-    const int n_tile = (GATED ? cx.nt * (BN / 2) + wn * (WN / 2) : cx.nt * BN + wn * WN) + q * 4;
-    const float* const scales = reinterpret_cast<const float*>(smem + scale_slot + parity * Slot::kBytes);
-    const float* const cols = scales + Slot::kRowLoads * 64 + q * 4;
+    const int n_tile = GATED ? cx.nt * (BN / 2) + wn * (WN / 2) : cx.nt * BN + wn * WN;
     constexpr int NO = GATED ? NJ / 2 : NJ;
     float rs[MI];
-#pragma unroll
-    for (int i = 0; i < MI; ++i) rs[i] = scales[i * 32 + r32];
+    read_row_scales(parity, rs);
 #pragma unroll
     for (int j = 0; j < NO; ++j) {
       f32x4 c0[4], c1[4];
-#pragma unroll
-      for (int vg = 0; vg < 4; ++vg) {
-        c0[vg] = *reinterpret_cast<const f32x4*>(cols + j * 32 + vg * 8);
-        if (GATED) c1[vg] = *reinterpret_cast<const f32x4*>(cols + Slot::kColLoads * 64 + j * 32 + vg * 8);
-      }
+      read_cols(parity, j * 32, c0);
+      if constexpr (GATED) read_cols(parity, Slot::kColLoads * 64 + j * 32, c1);
 #pragma unroll
       for (int i = 0; i < MI; ++i) {
-        const int row = (i * WGM + wm) * 32 + r32;
+        int l = lane;                                       // what depends on it is worked out anew, as in make_ctx
+        asm volatile("" : "+v"(l));
+        const int row = (i * WGM + wm) * 32 + (l & 31);
         if (row >= cx.row_count) continue;
         const size_t crow = (size_t)(cx.row_start + row);
 #pragma unroll
         for (int vg = 0; vg < 4; ++vg) {
-          const int n = n_tile + j * 32 + vg * 8;
+          const int n = n_tile + j * 32 + vg * 8 + (l >> 5) * 4;
           if (n >= p.N) continue;
           f32x4 o;
 #pragma unroll
@@ -510,9 +527,61 @@
       }
     }
   };
+  // The same through the strips of epilogue_staged, 32 rows x 64 columns.
+  auto epilogue_i8_staged = [&](const Ctx& cx, int parity) {
+    constexpr int kJ = 2;                                   // column subtiles of a strip
+    const uint32_t strip = (uint32_t)(uintptr_t)(lds_ptr_t)(smem + kStripBase) + wave * kStripBytes;
+    const uint32_t wr = strip + r32 * kStripPitch + q * 8;
+    float rs[MI];
+    read_row_scales(parity, rs);
+#pragma unroll
+    for (int j0 = 0; j0 < NJ; j0 += kJ) {
+      f32x4 c[kJ][4];
+#pragma unroll
+      for (int jl = 0; jl < kJ; ++jl) read_cols(parity, (j0 + jl) * 32, c[jl]);
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        const int row0 = (i * WGM + wm) * 32;
+        if (row0 >= cx.row_count) continue;                 // wavefront-uniform
+        __builtin_amdgcn_sched_barrier(0);                  // (as in epilogue_staged)
+        int l = lane;                                       // what depends on it is worked out anew, as in make_ctx
+        asm volatile("" : "+v"(l));
+        const int rd_row = l >> 3, rd_chunk = l & 7;        // + 8 t rows
+        const uint32_t rd = strip + rd_row * kStripPitch + rd_chunk * 16;
+#pragma unroll
+        for (int jl = 0; jl < kJ; ++jl)
+#pragma unroll
+          for (int vg = 0; vg < 4; ++vg) {
+            bf16x4 b;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) b[e] = (bf16_t)((float)acc[i][j0 + jl][vg * 4 + e] * (rs[i] * c[jl][vg][e]));
+            asm volatile("ds_write_b64 %0, %1 offset:%2" ::"v"(wr), "v"(__builtin_bit_cast(u32x2, b)), "n"(jl * 64 + vg * 16) : "memory");
+          }
+        u32x4 v0, v1, v2, v3;
+        asm volatile(
+            "ds_read_b128 %0, %4 offset:%5\n\tds_read_b128 %1, %4 offset:%6\n\t"
+            "ds_read_b128 %2, %4 offset:%7\n\tds_read_b128 %3, %4 offset:%8\n\ts_waitcnt lgkmcnt(0)"
+            : "=&v"(v0), "=&v"(v1), "=&v"(v2), "=&v"(v3)
+            : "v"(rd), "n"(0), "n"(8 * kStripPitch), "n"(16 * kStripPitch), "n"(24 * kStripPitch)
+            : "memory");
+        const u32x4 v[4] = {v0, v1, v2, v3};
+        const int col = cx.nt * BN + wn * WN + j0 * 32 + rd_chunk * 8;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const int row = row0 + t * 8 + rd_row;
+          if (row >= cx.row_count || col >= p.N) continue;
+          const size_t crow = (size_t)(cx.row_start + row);
+          if constexpr (DENSE) *reinterpret_cast<u32x4*>((uint16_t*)p.dense_out + crow * (size_t)p.dense_ldo + col) = v[t];
+          else *reinterpret_cast<u32x4*>(p.C + crow * p.N + col) = v[t];
+        }
+      }
+    }
+  };
   auto epilogue = [&](const Ctx& cx, int parity) {
     if constexpr (I8) {
-      epilogue_i8(cx, parity);
+      if constexpr (!kStagedStore) epilogue_i8(cx, parity);
+      else if (!DENSE || p.dense_vec == 2) epilogue_i8_staged(cx, parity);
+      else epilogue_i8(cx, parity);
     } else {
     if constexpr (SLICES) {
       // the accumulators as they are, an fp32 tile [BM][BN] in slot cx.part
