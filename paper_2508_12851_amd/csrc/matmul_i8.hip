@@ -1,8 +1,10 @@
 // out[m, n] = (sum_k aq[m, k] bq[n, k]) s_a[m] s_b[n] of two 8-bit matrices (prism.h): the grouped GEMM's kernel without groups
 // (grouped_gemm.h, DENSE).
 //
-// Few rows: the weights are streamed once, in 64 x 128 tiles, and the contraction of a tile is shared by several workgroups where
-// the tiles alone would leave compute units without one; they leave fp32 partial sums that a last kernel adds in their order.
+// Four tiles; where they alone would leave compute units without one, the contraction of a tile is shared by several workgroups,
+// which leave fp32 partial sums that a last kernel adds in their order.  Bound: large products by the power of the matrix
+// cores (8192 x 8192 x 8192 423 us, 2600 Tops; all zeros 298 us), few rows by streaming the weights, small ones by the latency of
+// their k-tiles.
 #include "grouped_gemm.h"
 
 namespace prism {
@@ -12,35 +14,55 @@ constexpr int kMaxSplits = 8;
 constexpr int kWorkgroups = 256;      // one per CU
 constexpr size_t kMaxPartialBytes = (size_t)64 << 20;
 
-enum class Tile { kFew, kSquare, kLarge };
+enum class Tile { k64x64, k64x128, k128x128, k256x256, kShort };
 struct Plan {
   Tile tile;
   int splits;
 };
 
-constexpr int kFewRows = 64;
-// What a tile's contraction costs to begin and end, in k-tiles of 64 bytes.
-constexpr float kRoundKt = 14.f;
+// The tile and the splits of a product, by an estimate of its time in us.  A round of items takes a fixed time and so much
+// per k-tile of 128 bytes, more as more workgroups share the L2: fitted to 20 products from 1 x 1024 x 4096 to 4096 x 4096 x 14336, weights
+// from HBM, of which each was run with all tiles and 1 to 8 splits.  Two 64 x 64 items share a CU, each then 1.5 times as long.
+// A split costs the kernel that adds the parts and their traffic; more workgroups than CUs by splits were slower everywhere.
+// Measured, us, 64 x 64 / 64 x 128 / 128 x 128 (best number of splits of each): 1 x 4096 x 14336 16.9 / 18.0; 64 x 14336 x 4096
+// 15.8 / 20.2; 128 x 14336 x 4096 23.7 / 19.8 / 23.9; 300 x 11008 x 4096 34.2 / 28.2 / 33.5; 600 x 4096 x 8192 59.5 / 49.5 / 36.5; 1000 x 4096 x
+// 4096 32.8 / 28.2 / 22.1 (256 x 256 39.7); 2000 x 4096 x 4096 64.1 / 52.0 / 40.0 (45.8).
+struct TileCost {
+  Tile tile;
+  int bm, bn, resident;     // resident: workgroups of a CU
+  float fixed, per_kt, per_kt_load;
+};
+constexpr TileCost kTiles[] = {{Tile::k64x64, 64, 64, 2, 3.6f, 0.27f, 0.01f},
+                               {Tile::k64x128, 64, 128, 1, 4.5f, 0.27f, 0.03f},
+                               {Tile::k128x128, 128, 128, 1, 4.5f, 0.34f, 0.18f},
+                               {Tile::k256x256, 256, 256, 1, 8.6f, 0.85f, 0.65f}};
+constexpr float kSplitFixed = 3.7f, kBytesPerUs = 5e6f, kStreamBytesPerUs = 6e6f;
+constexpr int kMinSplitKt = 3;        // k-tiles of a split, at least: the depth of the rings
 
 Plan plan_of(int M, int N, int K) {
-  const int kt = (int)(i8_row_bytes(K) / 64);
-  auto items = [&](int bm, int bn) { return (long long)ceil_div(M, bm) * ceil_div(N, bn); };
-  if (M > kFewRows && items(256, 256) >= kWorkgroups) return Plan{kt >= 3 ? Tile::kLarge : Tile::kSquare, 1};
-  const bool few = M <= kFewRows;
-  const long long n = few ? items(64, 128) : items(128, 128);
-  const int ring = few ? 7 : 6;       // k-tiles of 64 bytes that a split must have
-  int best = 1;
-  float cost = INFINITY;
-  for (int s = 1; s <= kMaxSplits; ++s) {
-    if (s > 1 && (kt / s < ring || (size_t)s * M * align_up(N, 4) * 4 > kMaxPartialBytes)) break;
-    const float rounds = (float)((n * s + kWorkgroups - 1) / kWorkgroups);
-    const float c = rounds * ((float)ceil_div(kt, s) + kRoundKt) + (s > 1 ? 12.f + 0.002f * (float)s * M * N / 4096.f : 0.f);
-    if (c < cost) {
-      cost = c;
-      best = s;
+  const int kt = (int)(i8_row_bytes(K) / 128);
+  if (kt < kMinSplitKt) return Plan{Tile::kShort, 1};
+  Plan best{Tile::k128x128, 1};
+  float least = INFINITY;
+  const float stream = (float)N * (float)K / kStreamBytesPerUs;
+  for (const TileCost& t : kTiles) {
+    const long long items = (long long)ceil_div(M, t.bm) * ceil_div(N, t.bn);
+    for (int s = 1; s <= kMaxSplits && (s == 1 || kt / s >= kMinSplitKt); ++s) {
+      const long long n = items * s;
+      if (s > 1 && (n > kWorkgroups || t.tile == Tile::k256x256 || (size_t)s * M * align_up(N, 4) * 4 > kMaxPartialBytes)) break;
+      float rounds = (float)((n + kWorkgroups - 1) / kWorkgroups);
+      if (t.resident == 2 && n > kWorkgroups) rounds = 1.5f * (float)((n + 2 * kWorkgroups - 1) / (2 * kWorkgroups));
+      const float load = std::min(1.f, (float)n / kWorkgroups);
+      const float loop = rounds * (t.fixed + (float)ceil_div(kt, s) * (t.per_kt + t.per_kt_load * load));
+      float us = std::max(loop, t.fixed + stream);
+      if (s > 1) us += kSplitFixed + 8.f * (float)s * (float)M * (float)N / kBytesPerUs;
+      if (us < least) {
+        least = us;
+        best = Plan{t.tile, s};
+      }
     }
   }
-  return Plan{few ? Tile::kFew : Tile::kSquare, best};
+  return best;
 }
 
 // out = sum of the splits' partial sums, in their order: four columns per thread.
@@ -61,12 +83,13 @@ __global__ __launch_bounds__(256) void reduce_dense_kernel(const float* __restri
   gg::store_dense(out, ldo, f32, vec, row, n, N, sum);
 }
 
-template <int BM, int BN, int BK, int STAGES, bool STREAM_B, bool CAN_SPLIT = true>
-prism_status launch_tiles(gg::GemmArgs& g, long long items, hipStream_t st) {
+template <int BM, int BN, int BK, int STAGES, bool CAN_SPLIT>
+prism_status launch_tiles(const gg::GemmArgs& g, hipStream_t st) {
+  const long long items = (long long)ceil_div(g.c_rows, BM) * ceil_div(g.N, BN);
   const int per_xcd = (int)((items + gg::kXcds - 1) / gg::kXcds);
   if constexpr (CAN_SPLIT)
-    if (g.dense_splits > 1) return gg::launch_gemm<BM, BN, 2, 2, BK, STAGES, false, true, STREAM_B, STREAM_B, false, true, true>(g, per_xcd, st);
-  return gg::launch_gemm<BM, BN, 2, 2, BK, STAGES, false, false, STREAM_B, STREAM_B, false, true, true>(g, per_xcd, st);
+    if (g.dense_splits > 1) return gg::launch_gemm<BM, BN, 2, 2, BK, STAGES, false, true, false, false, false, true, true>(g, per_xcd, st);
+  return gg::launch_gemm<BM, BN, 2, 2, BK, STAGES, false, false, false, false, false, true, true>(g, per_xcd, st);
 }
 
 }  // namespace
@@ -82,7 +105,7 @@ prism_status launch_matmul_i8(const void* a, const void* b, int M, int N, int K,
   if (M == 0) return PRISM_OK;
   constexpr size_t kMaxOperandBytes = 0xFFFF0000ull;    // 32-bit offsets
   if (i8_elements(M, K) >= kMaxOperandBytes || i8_elements(N, K) >= kMaxOperandBytes) return PRISM_ERR_UNSUPPORTED;
-  if ((long long)ceil_div(M, 64) * ceil_div(N, 128) >= (1LL << 30)) return PRISM_ERR_UNSUPPORTED;
+  if ((long long)ceil_div(M, 64) * ceil_div(N, 64) >= (1LL << 30)) return PRISM_ERR_UNSUPPORTED;
   const Plan plan = plan_of(M, N, K);
   gg::GemmArgs g{};
   g.A = (const uint16_t*)a;
@@ -103,20 +126,14 @@ prism_status launch_matmul_i8(const void* a, const void* b, int M, int N, int K,
   g.dense_f32 = out_dtype == PRISM_F32;
   const int es = g.dense_f32 ? 4 : 2;
   g.dense_vec = ((uintptr_t)out & (4 * es - 1)) == 0 && ldo % 4 == 0;
+  if (!g.dense_f32 && ((uintptr_t)out & 15) == 0 && ldo % 8 == 0 && N % 8 == 0) g.dense_vec = 2;
   g.dense_splits = plan.splits;
-  auto items = [&](int bm, int bn) { return (long long)ceil_div(M, bm) * ceil_div(N, bn); };
   switch (plan.tile) {
-    case Tile::kFew:
-      if (g.K / 32 >= 7) PRISM_TRY((launch_tiles<64, 128, 32, 8, true>(g, items(64, 128), st)));
-      else PRISM_TRY((launch_tiles<64, 128, 32, 3, true, false>(g, items(64, 128), st)));
-      break;
-    case Tile::kSquare:
-      if (g.K / 64 >= 3) PRISM_TRY((launch_tiles<128, 128, 64, 4, false>(g, items(128, 128), st)));
-      else PRISM_TRY((launch_tiles<128, 128, 32, 3, false, false>(g, items(128, 128), st)));
-      break;
-    case Tile::kLarge:
-      PRISM_TRY((launch_tiles<256, 256, 32, 4, false, false>(g, items(256, 256), st)));
-      break;
+    case Tile::k64x64: PRISM_TRY((launch_tiles<64, 64, 64, 4, true>(g, st))); break;
+    case Tile::k64x128: PRISM_TRY((launch_tiles<64, 128, 64, 4, true>(g, st))); break;
+    case Tile::k128x128: PRISM_TRY((launch_tiles<128, 128, 64, 4, true>(g, st))); break;
+    case Tile::k256x256: PRISM_TRY((launch_tiles<256, 256, 32, 4, false>(g, st))); break;
+    case Tile::kShort: PRISM_TRY((launch_tiles<128, 128, 32, 3, false>(g, st))); break;
   }
   if (plan.splits > 1) {
     const long long threads = (long long)M * (align_up(N, 4) / 4);
