@@ -18,7 +18,7 @@
 namespace prism {
 namespace {
 
-constexpr int kThreads = 512;           // of balance_kernel
+constexpr int kThreads = 1024;          // of balance_kernel
 constexpr int kFinishThreads = 1024;
 constexpr int kBackThreads = 256;
 constexpr int kMaxE = PRISM_MAX_EXPERTS;
@@ -254,22 +254,18 @@ struct BackwardArgs {
   int softmax_all;
 };
 
-// Slot j of a row's picks belongs to lane j % LPR of the row, register j / LPR; in rows of 16 lanes and more every 16 of them
-// hold all slots (a lane's value then reaches the 16 by one move inside the vector ALU, row_newbcast).
+// Slot j of a row's picks belongs to lane j % LPR of the row, register j / LPR; in rows of more than 16 lanes every 16 of them hold
+// all slots.  What a pick adds to its expert reaches the lane that has the expert through LDS, where a wavefront has a float per
+// expert of its rows (adding in the vector ALU, 8 slots to 4 experts per lane, took two fifths of the kernel's instructions).
 template <int LPR> constexpr int slots_of = LPR >= PRISM_MAX_TOPK ? 1 : PRISM_MAX_TOPK / LPR;
 template <int LPR> constexpr int slot_lanes_of = LPR > 16 ? 16 : LPR;
-template <int LPR, int J> __device__ __forceinline__ int slot_value(const int (&v)[slots_of<LPR>]) {
-  const int x = v[J / LPR];
-  if constexpr (LPR == 1) return x;
-  else if constexpr (LPR >= 16) return dpp_move<0x150 + J>(x, x);
-  else return __shfl(x, J % LPR, LPR);
-}
 
 template <int LPR>
 __global__ __launch_bounds__(kBackThreads) void route_backward_kernel(const BackwardArgs b) {
   constexpr int kRows = 64 / LPR, SL = slots_of<LPR>, kSlotLanes = slot_lanes_of<LPR>;
   constexpr int kAhead = back_ahead_of<LPR>, kWaves = kBackThreads / 64;
   const RowArgs& a = b.r;
+  __shared__ __align__(16) float s_add[kWaves][256];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int in_row = lane % LPR, e0 = in_row * 4;
   const Rows r = rows_of(a);
@@ -339,25 +335,18 @@ __global__ __launch_bounds__(kBackThreads) void route_backward_kernel(const Back
       }
       f32x4 g = {0.f, 0.f, 0.f, 0.f};       // of this lane's experts
       if (b.d_gate != nullptr) {
-        int bits[SL];
+        float* const add_to = s_add[wave];
+        *reinterpret_cast<f32x4*>(add_to + lane * 4) = f32x4{0.f, 0.f, 0.f, 0.f};
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        // (one wavefront's additions, of one instruction or one after the other: an expert picked twice gets its sum in the same
+        // order every time)
 #pragma unroll
-        for (int q = 0; q < SL; ++q) bits[q] = __float_as_int(t[q]);
-        auto add_slot = [&](auto j) {
-          if (j.value >= a.k) return;
-          const int d = slot_value<LPR, j.value>(idx[s]) - e0;
-          const float x = __int_as_float(slot_value<LPR, j.value>(bits));
-#pragma unroll
-          for (int i = 0; i < 4; ++i) g[i] += d == i ? x : 0.f;
-        };
-        add_slot(std::integral_constant<int, 0>{});
-        add_slot(std::integral_constant<int, 1>{});
-        add_slot(std::integral_constant<int, 2>{});
-        add_slot(std::integral_constant<int, 3>{});
-        add_slot(std::integral_constant<int, 4>{});
-        add_slot(std::integral_constant<int, 5>{});
-        add_slot(std::integral_constant<int, 6>{});
-        add_slot(std::integral_constant<int, 7>{});
-        static_assert(PRISM_MAX_TOPK == 8, "all slots");
+        for (int q = 0; q < SL; ++q)
+          if (in_row < kSlotLanes && idx[s][q] >= 0)
+            __hip_atomic_fetch_add(add_to + (lane - in_row) * 4 + idx[s][q], t[q], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        g = *reinterpret_cast<const f32x4*>(add_to + lane * 4);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       }
       f32x4 w = u;
       if (b.softmax_all) w += g;
@@ -395,7 +384,7 @@ template <typename Fn> void with_lanes(int E, Fn&& fn) {
   else fn(std::integral_constant<int, 64>{});
 }
 
-constexpr int kParts = 512;       // workgroups that share the tokens of a batch in balance_kernel, about
+constexpr int kParts = 256;       // workgroups that share the tokens of a batch in balance_kernel, about
 constexpr int kBackParts = 2048;  // ... and in route_backward_kernel, which leaves no sums to be added
 constexpr int kMaxGroups = PRISM_MAX_BALANCE_GROUPS;   // (a workgroup each: below 2^32 threads)
 

@@ -46,6 +46,9 @@ def backward(logits, idx, mask, group, E, k, d_loss, d_gate, mode):
             picks = idx[rows].reshape(-1)
             c = np.bincount(picks[(picks >= 0) & (picks < E)], minlength=E).astype(np.float64)
             u += float(d_loss[g]) * E / (k * n * n) * (c - c.mean())
+        # a rounded sum is off by EPS of the magnitudes of its terms at each addition, not of the sum: an expert picked more than once
+        # adds several gate gradients to u, which may cancel
+        u_size = np.abs(u)
         direct, direct_size = np.zeros((n, E)), np.zeros((n, E))
         if d_gate is not None:
             for t, row in enumerate(rows):
@@ -54,12 +57,13 @@ def backward(logits, idx, mask, group, E, k, d_loss, d_gate, mode):
                 es = idx[row, js]
                 if mode == "softmax_all":
                     np.add.at(u[t], es, dg)
+                    np.add.at(u_size[t], es, np.abs(dg))
                 elif js:
                     gate = softmax(l[t, es][None])[0]
                     np.add.at(direct[t], es, gate * (dg - gate @ dg))
                     np.add.at(direct_size[t], es, gate * (np.abs(dg) + gate @ np.abs(dg)))
         d[rows] = p * (u - (u * p).sum(axis=1, keepdims=True)) + direct
-        size[rows] = p * (np.abs(u) + (np.abs(u) * p).sum(axis=1, keepdims=True)) + direct_size
+        size[rows] = p * (u_size + (u_size * p).sum(axis=1, keepdims=True)) + direct_size
     return d, size
 
 

@@ -112,6 +112,20 @@ def test_experts_at_minus_infinity_and_rows_of_nothing_else(mode, E):
     _check(E, 2, 30, mode, logits, idx, None, d_loss, d_gate)
 
 
+@pytest.mark.parametrize("E", [4, 9, 20, 40, 128, 256])
+def test_an_expert_picked_many_times_gives_the_same_bits(E):
+    k = min(8, E)
+    logits, idx, _, d_loss, d_gate = _inputs(500, E, k, 0, False, E)
+    idx[:, 1:] = idx[:, :1]
+    idx[::3, k // 2] = (idx[::3, 0] + 1) % E
+    desc = P.make_desc(64, 64, E, k, gate_mode="softmax_all")
+    args = (desc, _dev(logits), _dev(idx))
+    first = P.prism_route_backward(*args, d_gate=_dev(d_gate))
+    for _ in range(5):
+        assert torch.equal(P.prism_route_backward(*args, d_gate=_dev(d_gate)), first)
+    _check(E, k, 0, "softmax_all", logits, idx, None, d_loss, d_gate)
+
+
 def test_near_even_spread_keeps_its_digits():
     """Counts that differ by one in 4096: the gradient is what the difference says, to fp32 precision."""
     T, E, k = 8192, 8, 4
