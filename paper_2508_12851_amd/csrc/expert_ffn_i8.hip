@@ -26,7 +26,6 @@ prism_status run_i8_ffn(const prism_layer_desc& d, const void* x, const prism_ex
   int32_t* const sched2 = ws.tiles + tile_table_ints(d, T);
   const FfnShapes f = shapes_of<C1, C2, SPLIT_DOWN, ROTATE, WIDTHS>(d, T);   // as ffn_schedule_shapes()
   constexpr bool kPrefill = !SPLIT_DOWN && C2::BM == 256;
-  if (!schedules_built) PRISM_TRY(gg::launch_build_schedules(d, local_offsets, T, ws.tiles, st));
 
   // Prefill tiles read 64 bytes of a row per k-tile, half a line of a gathered one: where a copy of the tokens in row order pays
   // for bf16 weights, they are quantised in row order into tiles (once per pick).  Other batches gather.
@@ -41,7 +40,8 @@ prism_status run_i8_ffn(const prism_layer_desc& d, const void* x, const prism_ex
     qx.local_src = local_src; qx.local_offsets = local_offsets;
     qx.E = d.n_experts; qx.A = A; qx.T = T; qx.top_k = d.top_k;
   }
-  PRISM_TRY(launch_quantize(qx, d.dtype, st));
+  if (schedules_built) PRISM_TRY(launch_quantize(qx, PRISM_BF16, st));
+  else PRISM_TRY(launch_quantize_tokens(d, qx, local_offsets, T, ws.tiles, st));
   trace(stage_events, PRISM_STAGE_DISPATCH, 1, st);   // counts as dispatch: its end is recorded anew
 
   GemmArgs g1{};

@@ -263,6 +263,9 @@ struct QuantizeArgs {
   int32_t* places;           // tiled: where each row starts in dst, in 64-byte units; or NULL
 };
 prism_status launch_quantize(const QuantizeArgs& a, int src_dtype, hipStream_t st);
+// bf16 tokens, and the schedules of the two products of an expert FFN (T tokens, lists as in launch_expert_ffn) in one launch.
+prism_status launch_quantize_tokens(const prism_layer_desc& d, const QuantizeArgs& a, const int32_t* local_offsets, int T,
+                                    int32_t* tiles, hipStream_t st);
 prism_status launch_pack_i8(const int8_t* src, long long ld, const float* scale, int rows, int cols, void* dst, hipStream_t st);
 
 // out = (a b^T) with the rows' scales (matmul_i8.hip).

@@ -12,7 +12,7 @@
 // (rows of more than 16384 elements are read again from there on).
 #include <type_traits>
 
-#include "prism_internal.h"
+#include "grouped_gemm.h"
 
 namespace prism {
 namespace {
@@ -177,12 +177,30 @@ __device__ __forceinline__ void quantize_row(const QuantizeArgs& a, int r, int l
 }
 
 template <typename S, bool VEC, int LANES, int HELD>
-__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void quantize_kernel(const QuantizeArgs a) {
+__device__ __forceinline__ void quantize_rows(const QuantizeArgs& a, int wg, int wgs) {
   if constexpr (LANES == 64) {
-    for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < a.rows; r += gridDim.x * 4)
-      quantize_row<S, VEC, 64, HELD>(a, r, threadIdx.x & 63);
+    for (int r = wg * 4 + (threadIdx.x >> 6); r < a.rows; r += wgs * 4) quantize_row<S, VEC, 64, HELD>(a, r, threadIdx.x & 63);
   } else {
-    for (int r = blockIdx.x; r < a.rows; r += gridDim.x) quantize_row<S, VEC, LANES, HELD>(a, r, threadIdx.x);
+    for (int r = wg; r < a.rows; r += wgs) quantize_row<S, VEC, LANES, HELD>(a, r, threadIdx.x);
+  }
+}
+
+template <typename S, bool VEC, int LANES, int HELD>
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void quantize_kernel(const QuantizeArgs a) {
+  quantize_rows<S, VEC, LANES, HELD>(a, blockIdx.x, gridDim.x);
+}
+
+// The tokens of an expert FFN, and the schedules of its two products: some workgroups more, where a launch of their own took 4 to 10 us.
+constexpr int kScheduleParts = 4;             // workgroups that share the items of one schedule
+template <int LANES, int HELD, bool WIDTHS>
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void quantize_and_schedule_kernel(
+    const QuantizeArgs a, const int32_t* __restrict__ local_offsets, int E, int S, int T, int A_total,
+    const gg::sched_params_t<WIDTHS> p0, const gg::sched_params_t<WIDTHS> p1) {
+  if (blockIdx.x < 2 * kScheduleParts) {
+    const gg::sched_params_t<WIDTHS> p[1] = {blockIdx.x < kScheduleParts ? p0 : p1};
+    gg::build_schedules_block<1, WIDTHS>(local_offsets, E, S, T, A_total, p, blockIdx.x % kScheduleParts, kScheduleParts);
+  } else {
+    quantize_rows<bf16_t, true, LANES, HELD>(a, blockIdx.x - 2 * kScheduleParts, gridDim.x - 2 * kScheduleParts);
   }
 }
 
@@ -212,29 +230,60 @@ __global__ __launch_bounds__(kThreads) void pack_i8_kernel(const int8_t* __restr
 
 }  // namespace
 
+namespace {
+// Calls launch(lanes, held) with the lanes of a row: a wavefront where rows are many and it holds them; else as many as make one or two
+// passes of it.  Bytes in and out, TB/s (a large copy reaches 4.8): 28000 x 1408 fp32 by 64 lanes 5.7, by 256 4.9; 600 x
+// 2048 bf16 4.4 against 3.6 us; 7200 x 4096 bf16 by 256 lanes 5.7, by 512 4.4; 4096 x 14336 bf16 by 512 lanes 5.7, by 1024 4.4, by
+// 256 5.2; 7200 x 14336 fp32 4.8 by any.
+template <typename Fn> void with_row_lanes(const QuantizeArgs& a, Fn&& launch) {
+  using std::integral_constant;
+  if (a.cols <= 2048 && a.rows > 4096) launch(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+  else if (a.cols <= 2048) launch(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+  else if (a.cols <= 4096) launch(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+  else if (a.rows > 512) launch(integral_constant<int, 512>{}, integral_constant<int, 4>{});
+  else launch(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+}
+template <typename S> bool rows_aligned(const QuantizeArgs& a) {
+  return ((uintptr_t)a.src & 15u) == 0 && a.ld * (long long)sizeof(S) % 16 == 0;
+}
+unsigned workgroups(const QuantizeArgs& a, int lanes) { return (unsigned)std::min(ceil_div(a.rows, lanes == 64 ? 4 : 1), kMaxGrid); }
+}  // namespace
+
 prism_status launch_quantize(const QuantizeArgs& a, int src_dtype, hipStream_t st) {
   if (a.rows == 0) return PRISM_OK;
-  auto launch = [&](auto elem, auto lanes, auto held) {
+  auto of_type = [&](auto elem) {
     using S = decltype(elem);
-    constexpr int kLanes = decltype(lanes)::value, kHeld = decltype(held)::value, kRows = kLanes == 64 ? 4 : 1;
-    const bool vec = ((uintptr_t)a.src & 15u) == 0 && a.ld * (long long)sizeof(S) % 16 == 0;
-    const dim3 grid((unsigned)std::min(ceil_div(a.rows, kRows), kMaxGrid)), block(kLanes * kRows);
-    if (vec) hipLaunchKernelGGL((quantize_kernel<S, true, kLanes, kHeld>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((quantize_kernel<S, false, kLanes, kHeld>), grid, block, 0, st, a);
+    with_row_lanes(a, [&](auto lanes, auto held) {
+      constexpr int L = decltype(lanes)::value, N = decltype(held)::value;
+      const dim3 grid(workgroups(a, L)), block(L < 256 ? 256 : L);
+      if (rows_aligned<S>(a)) hipLaunchKernelGGL((quantize_kernel<S, true, L, N>), grid, block, 0, st, a);
+      else hipLaunchKernelGGL((quantize_kernel<S, false, L, N>), grid, block, 0, st, a);
+    });
   };
-  // Lanes of a row: a wavefront where rows are many and it holds them; else as many as make one or two passes of it.  Bytes in and out,
-  // TB/s (a large copy reaches 4.8): 28000 x 1408 fp32 by 64 lanes 5.7, by 256 4.9; 600 x 2048 bf16 4.4 against 3.6 us; 7200 x 4096 bf16 by
-  // 256 lanes 5.7, by 512 4.4; 4096 x 14336 bf16 by 512 lanes 5.7, by 1024 4.4, by 256 5.2; 7200 x 14336 fp32 4.8 by any.
-  auto choose = [&](auto elem) {
-    using std::integral_constant;
-    if (a.cols <= 2048 && a.rows > 4096) launch(elem, integral_constant<int, 64>{}, integral_constant<int, 4>{});
-    else if (a.cols <= 2048) launch(elem, integral_constant<int, 256>{}, integral_constant<int, 1>{});
-    else if (a.cols <= 4096) launch(elem, integral_constant<int, 256>{}, integral_constant<int, 2>{});
-    else if (a.rows > 512) launch(elem, integral_constant<int, 512>{}, integral_constant<int, 4>{});
-    else launch(elem, integral_constant<int, 1024>{}, integral_constant<int, 2>{});
-  };
-  if (src_dtype == PRISM_F32) choose(float{});
-  else choose(bf16_t{});
+  if (src_dtype == PRISM_F32) of_type(float{});
+  else of_type(bf16_t{});
+  PRISM_CHECK_LAUNCH();
+  return PRISM_OK;
+}
+
+prism_status launch_quantize_tokens(const prism_layer_desc& d, const QuantizeArgs& a, const int32_t* local_offsets, int T,
+                                    int32_t* tiles, hipStream_t st) {
+  if (!rows_aligned<bf16_t>(a)) {     // (prism.h asks for aligned tokens)
+    PRISM_TRY(launch_quantize(a, PRISM_BF16, st));
+    return gg::launch_build_schedules(d, local_offsets, T, tiles, st);
+  }
+  gg::WidthParams p0, p1;
+  gg::ffn_sched_params(d, T, tiles, &p0, &p1);
+  with_row_lanes(a, [&](auto lanes, auto held) {
+    constexpr int L = decltype(lanes)::value, N = decltype(held)::value;
+    const dim3 grid(workgroups(a, L) + 2 * kScheduleParts), block(L < 256 ? 256 : L);
+    if (p0.wide_ntiles > 0)
+      hipLaunchKernelGGL((quantize_and_schedule_kernel<L, N, true>), grid, block, 0, st, a, local_offsets, d.n_experts, d.n_shared, T,
+                         T * d.top_k, p0, p1);
+    else
+      hipLaunchKernelGGL((quantize_and_schedule_kernel<L, N, false>), grid, block, 0, st, a, local_offsets, d.n_experts, d.n_shared, T,
+                         T * d.top_k, p0, p1);
+  });
   PRISM_CHECK_LAUNCH();
   return PRISM_OK;
 }
