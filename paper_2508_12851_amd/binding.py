@@ -117,9 +117,12 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 
 def _stream(stream: Optional[torch.cuda.Stream]) -> Optional[int]:
-    # (the stream object of the current device's stream takes 2.5 us to make)
-    s = torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) if stream is None else stream.cuda_stream
-    return s or None
+    return _stream_on(torch.cuda.current_device(), stream)
+
+
+def _stream_on(dev: int, stream: Optional[torch.cuda.Stream]) -> Optional[int]:
+    # (the stream object of a device's current stream takes 2.5 us to make)
+    return (torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream) or None
 
 
 def make_desc(hidden: int, ffn: int, n_experts: int, top_k: int, n_shared: int = 0,
@@ -195,16 +198,23 @@ def alloc_balance_workspace(desc: LayerDesc, device="cuda") -> torch.Tensor:
     return torch.empty(n.value, dtype=torch.uint8, device=device)
 
 
-def _typed(t: Optional[torch.Tensor], dtype: torch.dtype, shape: tuple, what: str) -> Optional[int]:
-    """The address of a tensor that has to be of this type and shape, on the device the call is enqueued on."""
+def _typed(t: Optional[torch.Tensor], dtype: torch.dtype, shape: tuple, dev: int, what: str) -> Optional[int]:
+    """The address of a tensor that has to be of this type and shape, on device `dev`, which the call is enqueued on."""
     if t is None:
         return None
-    if t.dtype != dtype or t.shape != shape:
+    if t.dtype is not dtype or t.shape != shape:
         raise PrismError(f"{what} has to be {dtype} {shape}, not {t.dtype} {tuple(t.shape)}")
-    if t.get_device() != torch.cuda.current_device():
+    if t.get_device() != dev:
         raise PrismError(f"{what} is on {t.device}, not on the current device")
     if not t.is_contiguous():
         raise PrismError(f"{what} has to be contiguous")
+    return t.data_ptr()
+
+
+def _bytes_on(t: torch.Tensor, dev: int, what: str) -> int:
+    """The address of a buffer of bytes on device `dev`."""
+    if t.get_device() != dev or not t.is_contiguous():
+        raise PrismError(f"{what} has to be a contiguous buffer on the current device")
     return t.data_ptr()
 
 
@@ -234,12 +244,13 @@ def prism_balance_loss(desc: LayerDesc, logits, topk_idx, workspace, token_mask=
         o = BalanceOut(new((G,), dtype=f32), new((G, E), dtype=i32), new((G, E), dtype=f32), new((G,), dtype=i32))
     if G == 0:                  # no tokens, no groups: nothing to address
         return o
+    dev = torch.cuda.current_device()
     _check(load_library().prism_balance_loss(
-        ctypes.byref(desc), _typed(logits, f32, (T, E), "logits"), _typed(topk_idx, i32, (T, k), "topk_idx"),
-        _typed(token_mask, torch.uint8, (T,), "token_mask"), group_tokens, T, _typed(o.loss, f32, (G,), "loss"),
-        _typed(o.counts, i32, (G, E), "counts"), _typed(o.probs, f32, (G, E), "probs"),
-        _typed(o.n_tokens, i32, (G,), "n_tokens"), _ptr(workspace), workspace.numel(), _stream(stream)),
-        "prism_balance_loss")
+        ctypes.byref(desc), _typed(logits, f32, (T, E), dev, "logits"), _typed(topk_idx, i32, (T, k), dev, "topk_idx"),
+        _typed(token_mask, torch.uint8, (T,), dev, "token_mask"), group_tokens, T, _typed(o.loss, f32, (G,), dev, "loss"),
+        _typed(o.counts, i32, (G, E), dev, "counts"), _typed(o.probs, f32, (G, E), dev, "probs"),
+        _typed(o.n_tokens, i32, (G,), dev, "n_tokens"), _bytes_on(workspace, dev, "workspace"), workspace.numel(),
+        _stream_on(dev, stream)), "prism_balance_loss")
     return o
 
 
@@ -256,13 +267,14 @@ def prism_route_backward(desc: LayerDesc, logits, topk_idx, balance: Optional[Ba
         d_logits = logits.new_empty((T, E), dtype=f32)
     if T == 0:
         return d_logits
+    dev = torch.cuda.current_device()
     _check(load_library().prism_route_backward(
-        ctypes.byref(desc), _typed(logits, f32, (T, E), "logits"), _typed(topk_idx, i32, (T, k), "topk_idx"),
-        _typed(token_mask, torch.uint8, (T,), "token_mask"), group_tokens, T,
-        None if balance is None else _typed(balance.counts, i32, (G, E), "counts"),
-        None if balance is None else _typed(balance.n_tokens, i32, (G,), "n_tokens"),
-        _typed(d_loss, f32, (G,), "d_loss"), _typed(d_gate, f32, (T, k), "d_gate"),
-        _typed(d_logits, f32, (T, E), "d_logits"), _stream(stream)), "prism_route_backward")
+        ctypes.byref(desc), _typed(logits, f32, (T, E), dev, "logits"), _typed(topk_idx, i32, (T, k), dev, "topk_idx"),
+        _typed(token_mask, torch.uint8, (T,), dev, "token_mask"), group_tokens, T,
+        None if balance is None else _typed(balance.counts, i32, (G, E), dev, "counts"),
+        None if balance is None else _typed(balance.n_tokens, i32, (G,), dev, "n_tokens"),
+        _typed(d_loss, f32, (G,), dev, "d_loss"), _typed(d_gate, f32, (T, k), dev, "d_gate"),
+        _typed(d_logits, f32, (T, E), dev, "d_logits"), _stream_on(dev, stream)), "prism_route_backward")
     return d_logits
 
 
@@ -491,6 +503,10 @@ class I8Matrix:
     rows: int
     cols: int
 
+    def __post_init__(self):
+        if self.data.numel() * self.data.element_size() < _i8_bytes(self.rows, self.cols):
+            raise PrismError(f"{self.data.numel()} bytes are too few for an 8-bit matrix of {self.rows} x {self.cols}")
+
     def values(self):
         """(int8 [rows, cols], scales [rows]): copies in plain order."""
         R, C = -(-self.rows // 16) * 16, -(-self.cols // 128) * 128
@@ -505,11 +521,11 @@ def _i8_bytes(rows: int, cols: int) -> int:
     return -(-(R * (-(-cols // 128) * 128) + 4 * R) // 256) * 256
 
 
-def _rows_ptr(t: torch.Tensor, dtypes, what: str):
-    """(address, elements from row to row) of a matrix whose rows are contiguous."""
-    if t.dim() != 2 or t.dtype not in dtypes:
-        raise PrismError(f"{what} has to be a device matrix of {' or '.join(map(str, dtypes))}")
-    if t.get_device() != torch.cuda.current_device():
+def _rows_ptr(t: torch.Tensor, dev: int, what: str):
+    """(address, elements from row to row) of a matrix on device `dev` whose rows are contiguous."""
+    if t.dim() != 2:
+        raise PrismError(f"{what} has to be a matrix")
+    if t.get_device() != dev:
         raise PrismError(f"{what} is on {t.device}, not on the current device")
     rows, cols = t.shape
     ld = cols
@@ -522,6 +538,15 @@ def _rows_ptr(t: torch.Tensor, dtypes, what: str):
     return t.data_ptr(), ld
 
 
+_FLOAT_DTYPES = {torch.float32: PRISM_F32, torch.bfloat16: PRISM_BF16}
+
+
+def _float_dtype(t: torch.Tensor, what: str) -> int:
+    if t.dtype not in _FLOAT_DTYPES:
+        raise PrismError(f"{what} has to be fp32 or bf16, not {t.dtype}")
+    return _FLOAT_DTYPES[t.dtype]
+
+
 def _out_i8(out: Optional[I8Matrix], rows: int, cols: int, like: torch.Tensor) -> I8Matrix:
     if out is None:
         return I8Matrix(like.new_empty((_i8_bytes(rows, cols),), dtype=torch.uint8), rows, cols)
@@ -532,21 +557,26 @@ def _out_i8(out: Optional[I8Matrix], rows: int, cols: int, like: torch.Tensor) -
 
 def prism_quantize_i8(src, out: Optional[I8Matrix] = None, stream=None) -> I8Matrix:
     """fp32 or bf16 rows -> 8 bits with a scale per row (see prism.h)."""
-    ptr, ld = _rows_ptr(src, (torch.float32, torch.bfloat16), "src")
+    dev = torch.cuda.current_device()
+    dtype = _float_dtype(src, "src")
+    ptr, ld = _rows_ptr(src, dev, "src")
     rows, cols = src.shape
     o = _out_i8(out, rows, cols, src)
-    _check(load_library().prism_quantize_i8(ptr, PRISM_F32 if src.dtype == torch.float32 else PRISM_BF16, ld, rows, cols,
-                                            _ptr(o.data), _stream(stream)), "prism_quantize_i8")
+    _check(load_library().prism_quantize_i8(ptr, dtype, ld, rows, cols, _bytes_on(o.data, dev, "out"), _stream_on(dev, stream)),
+           "prism_quantize_i8")
     return o
 
 
 def prism_pack_i8(q, scale, out: Optional[I8Matrix] = None, stream=None) -> I8Matrix:
     """int8 rows and their fp32 scales, as a checkpoint holds them -> the library's layout."""
-    ptr, ld = _rows_ptr(q, (torch.int8,), "q")
+    dev = torch.cuda.current_device()
+    if q.dtype != torch.int8:
+        raise PrismError(f"q has to be int8, not {q.dtype}")
+    ptr, ld = _rows_ptr(q, dev, "q")
     rows, cols = q.shape
     o = _out_i8(out, rows, cols, q)
-    _check(load_library().prism_pack_i8(ptr, ld, _typed(scale, torch.float32, (rows,), "scale"), rows, cols, _ptr(o.data),
-                                        _stream(stream)), "prism_pack_i8")
+    _check(load_library().prism_pack_i8(ptr, ld, _typed(scale, torch.float32, (rows,), dev, "scale"), rows, cols,
+                                        _bytes_on(o.data, dev, "out"), _stream_on(dev, stream)), "prism_pack_i8")
     return o
 
 
@@ -564,8 +594,10 @@ def prism_matmul_i8(a: I8Matrix, b: I8Matrix, workspace, out=None, dtype=torch.b
         out = b.data.new_empty((a.rows, b.rows), dtype=dtype)
     elif out.shape != (a.rows, b.rows):
         raise PrismError(f"out has to be {a.rows} x {b.rows}, not {tuple(out.shape)}")
-    ptr, ldo = _rows_ptr(out, (torch.float32, torch.bfloat16), "out")
-    _check(load_library().prism_matmul_i8(_ptr(a.data), _ptr(b.data), a.rows, b.rows, a.cols, ptr, ldo,
-                                          PRISM_F32 if out.dtype == torch.float32 else PRISM_BF16, _ptr(workspace),
-                                          workspace.numel(), _stream(stream)), "prism_matmul_i8")
+    dev = torch.cuda.current_device()
+    out_dtype = _float_dtype(out, "out")
+    ptr, ldo = _rows_ptr(out, dev, "out")
+    _check(load_library().prism_matmul_i8(_bytes_on(a.data, dev, "a"), _bytes_on(b.data, dev, "b"), a.rows, b.rows, a.cols, ptr, ldo,
+                                          out_dtype, _bytes_on(workspace, dev, "workspace"), workspace.numel(),
+                                          _stream_on(dev, stream)), "prism_matmul_i8")
     return out

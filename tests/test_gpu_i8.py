@@ -405,4 +405,6 @@ def test_binding_refuses_what_does_not_fit():
     with pytest.raises(P.PrismError):
         P.prism_quantize_i8(_rows(4, 64, BF16, 1), out=b)
     with pytest.raises(P.PrismError):
+        P.I8Matrix(a.data, 4, 129)
+    with pytest.raises(P.PrismError):
         P.prism_quantize_i8(torch.as_strided(_rows(1, 200, BF16, 1)[0], (4, 64), (32, 1)))   # rows that overlap
