@@ -176,12 +176,22 @@ __device__ __forceinline__ void quantize_row(const QuantizeArgs& a, int r, int l
   for (int c = c0 + HELD * kPass; c < row_bytes; c += kPass) store(c, load_chunk<S, VEC>(row, c, a.cols));
 }
 
+// The 16 rows of a tile belong to workgroups that the hardware deals to one XCD (workgroups 8 apart), whose L2 joins their 64-byte
+// pieces to whole lines: `per` workgroups a tile, of `wgs` in all (the last ones, too few for 8 tiles, in order).
+__device__ __forceinline__ int same_xcd(int wg, int per, int wgs) {
+  const int first = wg / (8 * per) * (8 * per), i = wg - first;
+  return first + 8 * per <= wgs ? first + i % 8 * per + i / 8 : wg;
+}
 template <typename S, bool VEC, int LANES, int HELD>
 __device__ __forceinline__ void quantize_rows(const QuantizeArgs& a, int wg, int wgs) {
   if constexpr (LANES == 64) {
-    for (int r = wg * 4 + (threadIdx.x >> 6); r < a.rows; r += wgs * 4) quantize_row<S, VEC, 64, HELD>(a, r, threadIdx.x & 63);
+    const int all = (a.rows + 3) / 4;
+    for (int w = wg; w < all; w += wgs) {
+      const int r = same_xcd(w, 4, all) * 4 + (threadIdx.x >> 6);
+      if (r < a.rows) quantize_row<S, VEC, 64, HELD>(a, r, threadIdx.x & 63);
+    }
   } else {
-    for (int r = wg; r < a.rows; r += wgs) quantize_row<S, VEC, LANES, HELD>(a, r, threadIdx.x);
+    for (int w = wg; w < a.rows; w += wgs) quantize_row<S, VEC, LANES, HELD>(a, same_xcd(w, 16, a.rows), threadIdx.x);
   }
 }
 
