@@ -412,7 +412,8 @@ prism_status prism_pack_weights(const void* src, int32_t rows, int32_t cols, voi
  *   in their order.)
  *   a  [m,k], b [n,k] 8-bit matrices;  out [m,n] of prism_dtype out_dtype, ldo elements from row to row, of which only
  *   the first n are written
- *   workspace  256-byte aligned, prism_matmul_i8_workspace_bytes(max_m, n, k) for every m <= max_m
+ *   workspace  256-byte aligned, prism_matmul_i8_workspace_bytes(max_m, n, k) for every m <= max_m; not for two calls
+ *   that may overlap in time
  * Errors: INVALID_ARG (NULL, misaligned, sizes < 1, a row longer than ld), UNSUPPORTED (more than 130944 columns; a or b of 4 GiB or
  * more in a product), WORKSPACE_TOO_SMALL.  No rows (m or rows of prism_quantize_i8 0) is PRISM_OK, with nothing launched.
  */

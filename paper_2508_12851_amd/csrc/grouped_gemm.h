@@ -144,8 +144,8 @@ constexpr int gemm_lds_unstaged() {
   return STAGES * (BM + BN) * BK * 2 + (GATED ? 4096 : 0) +           // ring + source-row slots
          (I8 ? 4 * 2 * ScaleSlot<BM * WGN / 4, BN / WGN, GATED>::kBytes : 0);
 }
-// 8-bit products go through the strips where there is room for them (h, as above, does not: gate/up of 4096 tokens of the
-// 4096 x 14336 layer 803 us against 821 through strips of 32 fp32 columns; the product of 8192 x 8192 x 4096 275 -> 228 us).
+// 8-bit products go through the strips where there is room for them: 8192 x 8192 x 4096 275 -> 228 us.  (h, as above, gains nothing:
+// gate/up of 4096 tokens of the 4096 x 14336 layer 821 us through strips of 32 fp32 columns, 804 to 826 without.)
 template <int BM, int BN, int WGN, int BK, int STAGES, bool GATED, bool SPLITK, bool SLICES>
 constexpr bool staged_store_i8() {
   return !SPLITK && !SLICES && !GATED && (BN / WGN / 32) % 2 == 0 &&

@@ -7,7 +7,7 @@ in a real decode step.  Sweeping the number of hosted experts per layer from 0 t
 build's analogue of the paper's Fig. 4: time of the local part of a layer and bytes that would
 cross the network, against the proportion of expert calls served remotely.
 
-    python -m paper_2508_12851_amd.decode_sweep [--layers 16] [--tokens 32] [--graph]
+    python -m paper_2508_12851_amd.decode_sweep [--layers 16] [--tokens 32] [--graph] [--weights int8]
 
 Weights are synthetic (N(0, 1/H), drawn on the GPU), popularity bias is the seeded Zipf bias of
 prism_inputs with one rank permutation per layer, masks host the most popular experts.
@@ -26,7 +26,7 @@ class Stack:
     """L layers resident in HBM: router, bias, all E experts (so any mask can be swept)."""
 
     def __init__(self, n_layers: int, T: int, H: int, F: int, E: int, k: int, zipf_s: float = 1.0,
-                 seed: int = 0):
+                 seed: int = 0, weights: str = "bf16"):
         import torch
 
         from prism_inputs import zipf_bias
@@ -35,7 +35,8 @@ class Stack:
 
         self.B, self.torch = B, torch
         self.L, self.T, self.H, self.F, self.E, self.k = n_layers, T, H, F, E, k
-        self.desc = B.make_desc(H, F, E, k, 0, "bf16", 0)
+        self.desc = B.make_desc(H, F, E, k, 0, "bf16", 0, weight_layout="int8" if weights == "int8" else "row_major")
+        load = (lambda w: B.prism_quantize_i8(w).data) if weights == "int8" else (lambda w: w)
         gen = torch.Generator(device="cuda").manual_seed(seed)
 
         def normal(shape, std):
@@ -50,7 +51,7 @@ class Stack:
             self.ranks.append(ranks)
             self.bias.append(torch.from_numpy(zipf_bias(ranks, zipf_s).reshape(1, E)
                                               .astype(np.float32)).cuda())
-            experts = [(normal((F, H), H ** -0.5), normal((F, H), H ** -0.5), normal((H, F), F ** -0.5))
+            experts = [tuple(load(w) for w in (normal((F, H), H ** -0.5), normal((F, H), H ** -0.5), normal((H, F), F ** -0.5)))
                        for _ in range(E)]
             self.tables.append(B.WeightTable(experts, []))
         self.x0 = normal((T, H), 1.0)
@@ -81,12 +82,12 @@ class Stack:
 
 
 def sweep(n_layers: int = 16, T: int = 32, H: int = 4096, F: int = 14336, E: int = 8, k: int = 2,
-          steps: int = 20, warmup: int = 3, use_graph: bool = False, seed: int = 0) -> List[Dict]:
+          steps: int = 20, warmup: int = 3, use_graph: bool = False, seed: int = 0, weights: str = "bf16") -> List[Dict]:
     import torch
 
-    st = Stack(n_layers, T, H, F, E, k, seed=seed)
+    st = Stack(n_layers, T, H, F, E, k, seed=seed, weights=weights)
     rows = []
-    es = 2
+    es = 1 if weights == "int8" else 2
     for n_local in range(E + 1):
         masks = st.masks_hosting(n_local)
         for _ in range(warmup):
@@ -117,7 +118,7 @@ def sweep(n_layers: int = 16, T: int = 32, H: int = 4096, F: int = 14336, E: int
             "remote_bytes_per_step": remote_bytes,
             "weight_bytes_streamed_per_step": weight_bytes,
             "hbm_gbs": weight_bytes / (ms * 1e-3) / 1e9,
-            "graph": bool(use_graph),
+            "graph": bool(use_graph), "weights": weights,
         })
     return rows
 
@@ -132,9 +133,11 @@ def main():
     ap.add_argument("--top-k", type=int, default=2)
     ap.add_argument("--steps", type=int, default=20)
     ap.add_argument("--graph", action="store_true", help="replay each step from a captured graph")
+    ap.add_argument("--weights", choices=("bf16", "int8"), default="bf16",
+                    help="int8: expert weights in 8 bits with a scale per output channel, made as the layers are loaded")
     a = ap.parse_args()
     for row in sweep(a.layers, a.tokens, a.hidden, a.ffn, a.experts, a.top_k, a.steps,
-                     use_graph=a.graph):
+                     use_graph=a.graph, weights=a.weights):
         print(json.dumps(row), flush=True)
 
 

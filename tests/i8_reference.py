@@ -38,3 +38,15 @@ def swiglu(x, gate, up, down):
     # the scale, and 4 roundings of each of at most 8 parts of the sum
     sums = (hq.abs() @ w.t()) * hs[:, None] * down[1].double()
     return y, turned + H_ERROR * y.abs() + 12 * EPS * sums
+
+
+# Layers of the expert FFN's tests.
+SHAPES = [
+    # H, F, E, k, S, T, hosted: every path of ffn_paths.h, ragged tiles, one token, experts with no row
+    (64, 64, 4, 1, 0, 1, range(4)), (64, 64, 8, 2, 1, 65, range(0, 8, 2)), (128, 192, 8, 2, 2, 33, range(5)), (192, 448, 8, 2, 0, 64, range(8)),
+    (512, 2048, 8, 2, 0, 1, range(8)), (512, 2048, 8, 2, 1, 37, (0, 3, 4)), (512, 2048, 8, 2, 0, 66, range(8)), (512, 2048, 8, 2, 0, 200, (1,)),
+    (512, 2048, 8, 2, 0, 256, range(5)), (512, 2048, 8, 2, 1, 300, range(5)), (2880, 2048, 8, 2, 0, 500, range(3)), (1024, 1408, 60, 4, 2, 90, range(0, 60, 2)),
+    (1024, 1408, 60, 4, 2, 333, range(30)), (384, 384, 64, 6, 0, 100, range(64)), (256, 320, 8, 2, 1, 700, range(4)),
+    (320, 8192, 4, 2, 0, 600, range(3)), (256, 8256, 8, 2, 0, 400, (7,)), (1024, 512, 8, 2, 0, 1500, range(8)), (64, 1024, 4, 4, 0, 300, range(4)),
+    (384, 1024, 8, 2, 0, 20, range(8)), (1024, 8192, 4, 2, 1, 900, range(4)),
+]

@@ -147,6 +147,36 @@ def test_no_tokens():
     assert P.prism_route_backward(desc, logits, idx, b, torch.ones(1, device="cuda")).shape == (0, 8)
 
 
+def test_beyond_4_gib_of_logits():
+    T, E, k = 4_500_001, 256, 2
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    logits = torch.randn((T, E), generator=gen, device="cuda")
+    idx = torch.randint(0, E, (T, k), generator=gen, device="cuda").int()
+    desc = P.make_desc(64, 64, E, k)
+    b = P.prism_balance_loss(desc, logits, idx, P.alloc_balance_workspace(desc), group_tokens=3_000_000)
+    assert torch.equal(b.counts[0].long(), torch.bincount(idx[:3_000_000].reshape(-1), minlength=E))
+    assert torch.equal(b.counts[1].long(), torch.bincount(idx[3_000_000:].reshape(-1), minlength=E))
+    p = sum(torch.softmax(part.double(), 1).sum(0) for part in logits[3_000_000:].split(100_000)) / 1_500_001
+    # the derived error of a p, and one addition per row of a lane in fp32 (each of half an ulp of the sum so far)
+    lane_rows = -(-3_000_000 // 128) // 16 + 1
+    assert bool(((b.probs[1].double() - p).abs() <= (R.relative_error_of_p(12.0) + lane_rows * R.EPS) * p).all())
+    d = P.prism_route_backward(desc, logits, idx, b, torch.ones(2, device="cuda"), torch.ones((T, k), device="cuda"), group_tokens=3_000_000)
+    rows = torch.cat([torch.arange(0, T, 40009), torch.arange(T - 50, T)])
+    l, i = logits[rows.cuda()].cpu().numpy(), idx[rows.cuda()].cpu().numpy()
+    group = (rows >= 3_000_000).long().numpy()
+    n, c = np.array([3_000_000, 1_500_001]), b.counts.cpu().numpy().astype(np.float64)
+    u = (E * (c - c.mean(1, keepdims=True)) / (k * n * n.astype(float))[:, None])[group]
+    pr = R.softmax(l.astype(np.float64))
+    want = pr * (u - (u * pr).sum(1, keepdims=True))
+    size = pr * (np.abs(u) + (np.abs(u) * pr).sum(1, keepdims=True))
+    for t in range(len(rows)):
+        gate = R.softmax(l[t, i[t]][None].astype(np.float64))[0]
+        np.add.at(want[t], i[t], gate * (1.0 - gate.sum()))
+        np.add.at(size[t], i[t], 2 * gate)
+    err = np.abs(d[rows.cuda()].cpu().numpy() - want)
+    assert np.all(err <= (2 * R.relative_error_of_p(12.0) + 12 * R.EPS) * size + 1e-38)
+
+
 def test_same_bits_every_time_on_streams_and_in_graphs():
     T, E, k = 30011, 64, 6
     logits, idx, mask, d_loss, d_gate = (_dev(a) for a in _inputs(T, E, k, 0, True, 2))

@@ -240,14 +240,7 @@ class Layer:
         assert bool((y[at[-1]:T * self.k] == 0).all())
 
 
-SHAPES = [
-    # H, F, E, k, S, T, hosted: every path of ffn_paths.h, ragged tiles, one token, experts with no row
-    (64, 64, 4, 1, 0, 1, range(4)), (64, 64, 8, 2, 1, 65, range(0, 8, 2)), (128, 192, 8, 2, 2, 33, range(5)), (192, 448, 8, 2, 0, 64, range(8)),
-    (512, 2048, 8, 2, 0, 1, range(8)), (512, 2048, 8, 2, 1, 37, (0, 3, 4)), (512, 2048, 8, 2, 0, 66, range(8)), (512, 2048, 8, 2, 0, 200, (1,)),
-    (512, 2048, 8, 2, 0, 256, range(5)), (512, 2048, 8, 2, 1, 300, range(5)), (2880, 2048, 8, 2, 0, 500, range(3)), (1024, 1408, 60, 4, 2, 90, range(0, 60, 2)),
-    (1024, 1408, 60, 4, 2, 333, range(30)), (384, 384, 64, 6, 0, 100, range(64)), (256, 320, 8, 2, 1, 700, range(4)),
-    (320, 8192, 4, 2, 0, 600, range(3)), (256, 8256, 8, 2, 0, 400, (7,)), (1024, 512, 8, 2, 0, 1500, range(8)), (64, 1024, 4, 4, 0, 300, range(4)),
-]
+SHAPES = R.SHAPES
 
 
 @pytest.mark.parametrize("H,F,E,k,S,T,hosted", SHAPES)
@@ -355,6 +348,71 @@ def test_layer_in_a_graph_and_on_two_streams(T):
         got = out.out.clone()
         step(outs[0], wss[0])
         assert torch.equal(outs[0].out, got)
+
+
+def test_no_tokens():
+    layer = Layer(256, 512, 8, 2, 1, 0, range(8))
+    o = P.prism_moe_layer(layer.desc, layer.x, layer.router, layer.bias, layer.table, layer.mask, layer.ws)
+    assert o.out.shape == (0, 256) and int(o.counts.sum()) == 0
+
+
+def test_layer_with_stage_events():
+    import ctypes
+    layer = Layer(512, 2048, 8, 2, 1, 40, range(5), seed=3)
+    want = P.prism_moe_layer(layer.desc, layer.x, layer.router, layer.bias, layer.table, layer.mask, layer.ws)
+    events = [torch.cuda.Event(enable_timing=True) for _ in range(2 * len(P.STAGES))]
+    for e in events:
+        e.record()                                # (makes the handles)
+    handles = (ctypes.c_void_p * len(events))(*[e.cuda_event for e in events])
+    got = P.prism_moe_layer(layer.desc, layer.x, layer.router, layer.bias, layer.table, layer.mask, layer.ws, stage_events=handles)
+    torch.cuda.synchronize()
+    assert torch.equal(got.out, want.out)
+    assert all(events[2 * i].elapsed_time(events[2 * i + 1]) >= 0 for i in range(len(P.STAGES)))
+
+
+def test_decode_loop_with_8_bit_experts():
+    from paper_2508_12851_amd.decode_sweep import Stack, sweep
+    st = Stack(n_layers=2, T=24, H=256, F=512, E=8, k=2, seed=5, weights="int8")
+    ref = Stack(n_layers=2, T=24, H=256, F=512, E=8, k=2, seed=5)
+    masks = st.masks_hosting(8)
+    got, want = st.step(masks).double(), ref.step(masks).double()
+    # Weights, tokens and h in 8 bits: a row's step is its largest value / 127, 3.5 rms / 127 in a normal row of 256 or 512, 8 rms / 127 in
+    # one of h, and its rounding errors are 0.29 steps: 0.8 % of each of x and the weights, 1.8 % of h, together below 3 % of a
+    # layer's output, which is no larger than the x it is added to.
+    assert float((got - want).norm() / want.norm()) < 0.05
+    rows = sweep(n_layers=2, T=16, H=256, F=512, E=8, k=2, steps=2, warmup=1, weights="int8")
+    assert rows[-1]["weight_bytes_streamed_per_step"] % (3 * 256 * 512) == 0 and rows[-1]["weights"] == "int8"
+
+
+# ---- beyond 32-bit offsets ---------------------------------------------------------------------
+def test_h_beyond_4_gib():
+    T, H, F, E, k = 40000, 256, 14336, 4, 2
+    layer = Layer(H, F, E, k, 0, T, range(E), seed=4)
+    _, s = layer.route()
+    y = P.prism_expert_ffn(layer.desc, layer.x, layer.table, s.local_src, s.local_offsets, layer.ws)
+    at = s.local_offsets.tolist()
+    assert at[-1] * F * 4 > 1 << 32
+    for e in range(E):                            # the first, the last and some rows of every expert
+        rows = torch.unique(torch.cat([torch.tensor([at[e], at[e + 1] - 1]), torch.randint(at[e], at[e + 1], (60,), generator=torch.Generator().manual_seed(e))])).cuda()
+        want, off = R.swiglu(layer.x[s.local_src[rows].long() // k], *(m.values() for m in layer.experts[e]))
+        err = (y[rows].double() - want).abs()
+        assert bool((err <= 2.0 ** -8 * (want.abs() + off) + off).all())
+
+
+def test_product_and_quantisation_beyond_4_gib():
+    m, n, k = 300001, 4096, 128
+    v = _rows(m, k, BF16, 1)
+    w, ws = _weights(n, k, 2)
+    out = P.prism_matmul_i8(P.prism_quantize_i8(v), P.prism_pack_i8(w, ws), P.alloc_matmul_i8_workspace(m, n, k), dtype=F32)
+    rows = torch.cat([torch.arange(0, m, 1009), torch.arange(m - 40, m)]).cuda()
+    q, scale = R.quantize(v[rows])
+    want = R.product(q, scale, w, ws)
+    sums = (q.abs() @ w.double().abs().t()) * scale[:, None] * ws.double()
+    assert bool(((out[rows].double() - want).abs() <= 4 * R.EPS * sums + R.EPS * want.abs() * (1 + 2.0 ** -8)).all())
+    quantised = P.prism_quantize_i8(out)          # 4.9 GB in
+    q, scale = quantised.values()
+    want, want_scale = R.quantize(out[rows])
+    assert torch.equal(q[rows].double(), want) and torch.equal(scale[rows].double(), want_scale)
 
 
 def test_router_and_experts_of_a_training_step():

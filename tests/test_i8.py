@@ -4,7 +4,8 @@ import ctypes
 import pytest
 
 import paper_2508_12851_amd as P
-from ffn_paths import ffn_path
+import i8_reference as R
+from ffn_paths import cuts_last_round, ffn_path, packs_rows
 
 P0 = ctypes.c_void_p(0x10000)       # never dereferenced
 
@@ -111,3 +112,10 @@ def test_tile_rules_of_the_usual_sizes():
     assert ffn_path(2048, 1408, 60, 4, 4, 333, 2) == "kFewRows128"
     assert ffn_path(4096, 14336, 8, 2, 0, 4096, 2) == "kPrefill"
     assert ffn_path(64, 64, 8, 2, 0, 65, 2) == "kPrefillShort"
+
+
+def test_the_layers_of_the_tests_reach_every_path():
+    at = [(H, F, E, k, S, T, 2) for H, F, E, k, S, T, _ in R.SHAPES]
+    assert {ffn_path(*a) for a in at} == {"kDecodeTiled", "kDecode", "kDecodeShort", "kStream", "kSplitSquare", "kSplitWide",
+                                          "kFewRows64", "kFewRows128", "kPrefill", "kPrefillShort"}
+    assert any(packs_rows(*a) for a in at) and any(cuts_last_round(*a) for a in at)
