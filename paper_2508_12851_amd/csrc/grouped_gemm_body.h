@@ -583,74 +583,74 @@
       else if (!DENSE || p.dense_vec == 2) epilogue_i8_staged(cx, parity);
       else epilogue_i8(cx, parity);
     } else {
-    if constexpr (SLICES) {
-      // the accumulators as they are, an fp32 tile [BM][BN] in slot cx.part
-      float* tile = p.Cpart + (size_t)cx.part * (BM * BN);
+      if constexpr (SLICES) {
+        // the accumulators as they are, an fp32 tile [BM][BN] in slot cx.part
+        float* tile = p.Cpart + (size_t)cx.part * (BM * BN);
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+          if ((i * WGM + wm) * 32 >= cx.row_count) continue;    // wave-uniform
+          const int row = (i * WGM + wm) * 32 + r32;
+#pragma unroll
+          for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int vg = 0; vg < 4; ++vg) {
+              const int n = wn * WN + j * 32 + vg * 8 + q * 4;
+              const f32x4 o = {acc[i][j][vg * 4], acc[i][j][vg * 4 + 1], acc[i][j][vg * 4 + 2],
+                               acc[i][j][vg * 4 + 3]};
+              *reinterpret_cast<f32x4*>(tile + (size_t)row * BN + n) = o;
+            }
+        }
+        return;
+      }
+      if constexpr (kStagedStore) {
+        epilogue_staged(cx);
+        return;
+      }
 #pragma unroll
       for (int i = 0; i < MI; ++i) {
-        if ((i * WGM + wm) * 32 >= cx.row_count) continue;    // wave-uniform
         const int row = (i * WGM + wm) * 32 + r32;
+        if (row >= cx.row_count) continue;
+        const size_t crow = (size_t)(cx.row_start + row);
+        if (GATED) {
+          constexpr int NH = NJ / 2;
+          const int f0 = cx.nt * (BN / 2) + wn * (WN / 2);       // a multiple of 32
+          uint16_t* const out = p.C + (p.c_tiled ? (crow >> 4) * (size_t)(p.N >> 5) * 512 + (size_t)(f0 >> 5) * 512 +
+                                                       (crow & 15) * 32
+                                                 : crow * p.N + f0) + q * 4;
+          const int col_step = p.c_tiled ? 512 : 32;             // elements from one column subtile to the next
 #pragma unroll
-        for (int j = 0; j < NJ; ++j)
+          for (int j = 0; j < NH; ++j)
 #pragma unroll
-          for (int vg = 0; vg < 4; ++vg) {
-            const int n = wn * WN + j * 32 + vg * 8 + q * 4;
-            const f32x4 o = {acc[i][j][vg * 4], acc[i][j][vg * 4 + 1], acc[i][j][vg * 4 + 2],
-                             acc[i][j][vg * 4 + 3]};
-            *reinterpret_cast<f32x4*>(tile + (size_t)row * BN + n) = o;
-          }
-      }
-      return;
-    }
-    if constexpr (kStagedStore) {
-      epilogue_staged(cx);
-      return;
-    }
-#pragma unroll
-    for (int i = 0; i < MI; ++i) {
-      const int row = (i * WGM + wm) * 32 + r32;
-      if (row >= cx.row_count) continue;
-      const size_t crow = (size_t)(cx.row_start + row);
-      if (GATED) {
-        constexpr int NH = NJ / 2;
-        const int f0 = cx.nt * (BN / 2) + wn * (WN / 2);       // a multiple of 32
-        uint16_t* const out = p.C + (p.c_tiled ? (crow >> 4) * (size_t)(p.N >> 5) * 512 + (size_t)(f0 >> 5) * 512 +
-                                                     (crow & 15) * 32
-                                               : crow * p.N + f0) + q * 4;
-        const int col_step = p.c_tiled ? 512 : 32;             // elements from one column subtile to the next
-#pragma unroll
-        for (int j = 0; j < NH; ++j)
-#pragma unroll
-          for (int vg = 0; vg < 4; ++vg) {
-            if (f0 + j * 32 + vg * 8 + q * 4 < p.N) {
-              bf16x4 o;
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                o[e] = (bf16_t)(silu(acc[i][j][vg * 4 + e]) * acc[i][j + NH][vg * 4 + e]);
-              *reinterpret_cast<bf16x4*>(out + j * col_step + vg * 8) = o;
-            }
-          }
-      } else {
-#pragma unroll
-        for (int j = 0; j < NJ; ++j)
-#pragma unroll
-          for (int vg = 0; vg < 4; ++vg) {
-            const int n = cx.nt * BN + wn * WN + j * 32 + vg * 8 + q * 4;
-            if (n < p.N) {
-              if (SPLITK) {
-                const f32x4 o = {acc[i][j][vg * 4], acc[i][j][vg * 4 + 1], acc[i][j][vg * 4 + 2],
-                                 acc[i][j][vg * 4 + 3]};
-                *reinterpret_cast<f32x4*>(p.Cpart + ((size_t)split * p.c_rows + crow) * p.N + n) = o;
-              } else {
+            for (int vg = 0; vg < 4; ++vg) {
+              if (f0 + j * 32 + vg * 8 + q * 4 < p.N) {
                 bf16x4 o;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = (bf16_t)acc[i][j][vg * 4 + e];
-                *reinterpret_cast<bf16x4*>(p.C + crow * p.N + n) = o;
+                for (int e = 0; e < 4; ++e)
+                  o[e] = (bf16_t)(silu(acc[i][j][vg * 4 + e]) * acc[i][j + NH][vg * 4 + e]);
+                *reinterpret_cast<bf16x4*>(out + j * col_step + vg * 8) = o;
               }
             }
-          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int vg = 0; vg < 4; ++vg) {
+              const int n = cx.nt * BN + wn * WN + j * 32 + vg * 8 + q * 4;
+              if (n < p.N) {
+                if (SPLITK) {
+                  const f32x4 o = {acc[i][j][vg * 4], acc[i][j][vg * 4 + 1], acc[i][j][vg * 4 + 2],
+                                   acc[i][j][vg * 4 + 3]};
+                  *reinterpret_cast<f32x4*>(p.Cpart + ((size_t)split * p.c_rows + crow) * p.N + n) = o;
+                } else {
+                  bf16x4 o;
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) o[e] = (bf16_t)acc[i][j][vg * 4 + e];
+                  *reinterpret_cast<bf16x4*>(p.C + crow * p.N + n) = o;
+                }
+              }
+            }
+        }
       }
-    }
     }
   };
 
