@@ -10,7 +10,7 @@
 //
 // Rows: a token's E logits lie on 2^n lanes with 4 consecutive experts each, so that a wavefront holds one row of 256
 // experts or 64 rows of 4, and row sums are exchanges between lanes.  Both passes read the logits once: 65531 tokens of 256
-// experts (67 MB) 20 us for the sums (3.4 TB/s) and 12 to add their 256 parts, 36 us for the gradient (3.7 TB/s in and out; a
+// experts (67 MB) 20 us for the sums (3.4 TB/s) and 8 to add their 256 parts, 36 us for the gradient (3.7 TB/s in and out; a
 // large copy reaches 4.8): the vector ALU, about 100 and 210 instructions a row, takes nearly as long as memory.  Below a few MB the
 // launches' latency: 8192 tokens of 64 experts in 16 groups 10 + 5 us.
 #include <type_traits>
@@ -120,17 +120,28 @@ __device__ __forceinline__ void finish_group(int g, int E, int k, int n, int cou
 
 static_assert(kThreads >= kMaxE, "a thread per expert");
 
-// Partial sums of `parts` workgroups: probabilities [parts][E4], counts [parts][E4], tokens [parts], with E4 = E rounded up to 4.
+// What workgroups leave for one another.  Of the workgroups of balance_kernel: probabilities [kParts][E4], counts [kParts][E4] and
+// tokens [kParts], with E4 = E rounded up to 4; of those of finish_kernel: their shares of a group's loss [kParts][kMaxPieces],
+// and how many of a group's have left theirs [kParts].  (Groups that have parts are fewer than kParts.)
+constexpr int kParts = 256;       // workgroups that share the tokens of a batch in balance_kernel, about
+constexpr int kPieceLanes = 8;    // experts of a workgroup of finish_kernel, by fours
+constexpr int kMaxPieces = kMaxE / 4 / kPieceLanes;
 struct Partial {
+  double* terms;
   float* probs;
   int* counts;
   int* n;
+  unsigned* done;
   int E4;
 };
-__host__ __device__ inline Partial partial_of(void* base, int parts, int E) {
-  const int E4 = (E + 3) / 4 * 4;
-  float* const p = (float*)base;
-  return Partial{p, (int*)p + (size_t)parts * E4, (int*)p + (size_t)parts * E4 * 2, E4};
+size_t partial_bytes(int E) { return (size_t)kParts * (kMaxPieces * 8 + 2 * align_up(E, 4) * 4 + 2 * 4); }
+Partial partial_of(void* base, int E) {
+  const int E4 = (int)align_up(E, 4);
+  double* const terms = (double*)base;
+  float* const probs = (float*)(terms + kParts * kMaxPieces);
+  int* const counts = (int*)probs + (size_t)kParts * E4;
+  int* const n = counts + (size_t)kParts * E4;
+  return Partial{terms, probs, counts, n, (unsigned*)n + kParts, E4};
 }
 
 // Sums over a part of a group's tokens.  parts == 1: the group's results; else partial sums for finish_kernel.  A lane adds the
@@ -196,52 +207,91 @@ __global__ __launch_bounds__(kThreads) void balance_kernel(const RowArgs a, cons
     finish_group(r.group, a.E, a.k, s_n, tid < kMaxE ? s_counts[tid] : 0, total, counts, probs, n_tokens, loss);
     return;
   }
-  if (tid == 0) partial.n[blockIdx.x] = s_n;
+  if (tid == 0) {
+    partial.n[blockIdx.x] = s_n;
+    if (r.part == 0) partial.done[r.group] = 0;
+  }
   if (tid < partial.E4) {                   // (past E: zeros)
     partial.counts[(size_t)blockIdx.x * partial.E4 + tid] = s_counts[tid];
     partial.probs[(size_t)blockIdx.x * partial.E4 + tid] = total;
   }
 }
 
-// The parts of a group, added in 64 bits: thread (slice, 4 experts) the parts slice, slice + slices, ..., then pairs of slices.
-__global__ __launch_bounds__(kFinishThreads) void finish_kernel(const Partial partial, int E, int k, int parts, int lanes,
+// The parts of a group, added in 64 bits: thread (slice, 4 experts) the parts slice, slice + slices, ..., then the slices of a
+// wavefront, then the wavefronts.  `pieces` workgroups of 4 * lanes experts each share a group (256 parts of 256 experts: 8 us by 8
+// of them, 12 by one); the last of them to arrive adds their shares of the loss, in their order.
+__global__ __launch_bounds__(kFinishThreads) void finish_kernel(const Partial partial, int E, int k, int parts, int lanes, int pieces,
                                                                 int32_t* __restrict__ counts, float* __restrict__ probs,
                                                                 int32_t* __restrict__ n_tokens, float* __restrict__ loss) {
-  __shared__ double s_sum[kFinishThreads][4];
-  __shared__ int s_count[kFinishThreads][4], s_n[kFinishThreads];
-  const int tid = threadIdx.x, g = blockIdx.x;
-  const int slices = kFinishThreads / lanes, slice = tid / lanes, e0 = tid % lanes * 4;
+  constexpr int kWaves = kFinishThreads / 64;
+  __shared__ double s_sum[kWaves][kPieceLanes * 4];
+  __shared__ int s_count[kWaves][kPieceLanes * 4], s_n[kWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = blockIdx.x / pieces, piece = blockIdx.x % pieces;
+  const int first = piece * lanes * 4;
+  const int slices = kFinishThreads / lanes, slice = tid / lanes, e0 = first + tid % lanes * 4;
   double sum[4] = {0., 0., 0., 0.};
   int count[4] = {0, 0, 0, 0}, n = 0;
-  if (e0 < E)
 #pragma unroll 8
-    for (int p = slice; p < parts; p += slices) {
-      const size_t at = (size_t)g * parts + p;
-      n += partial.n[at];
+  for (int p = slice; p < parts; p += slices) {
+    const size_t at = (size_t)g * parts + p;
+    n += partial.n[at];
+    if (e0 < E) {
       const int4 c = *reinterpret_cast<const int4*>(partial.counts + at * partial.E4 + e0);
       const f32x4 v = *reinterpret_cast<const f32x4*>(partial.probs + at * partial.E4 + e0);
       count[0] += c.x; count[1] += c.y; count[2] += c.z; count[3] += c.w;
 #pragma unroll
       for (int i = 0; i < 4; ++i) sum[i] += (double)v[i];
     }
-  for (int half = slices; half > 0; half >>= 1) {   // the first round only writes
-    if (slice < half) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (half < slices) {
-          sum[i] += s_sum[tid + half * lanes][i];
-          count[i] += s_count[tid + half * lanes][i];
-        }
-        s_sum[tid][i] = sum[i];
-        s_count[tid][i] = count[i];
-      }
-      if (half < slices) n += s_n[tid + half * lanes];
-      s_n[tid] = n;
-    }
-    __syncthreads();
   }
-  finish_group(g, E, k, s_n[0], tid < E ? s_count[tid / 4][tid % 4] : 0, tid < E ? s_sum[tid / 4][tid % 4] : 0.0,
-                               counts, probs, n_tokens, loss);
+  for (int off = lanes; off < 64; off <<= 1) {
+    n += __shfl_xor(n, off);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      sum[i] += __shfl_xor(sum[i], off);
+      count[i] += __shfl_xor(count[i], off);
+    }
+  }
+  if (lane < lanes)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      s_sum[wave][lane * 4 + i] = sum[i];
+      s_count[wave][lane * 4 + i] = count[i];
+    }
+  if (lane == 0) s_n[wave] = n;
+  __syncthreads();
+  if (wave != 0) return;
+  static_assert(kPieceLanes * 4 <= 64, "a wavefront has a thread per expert of a piece");
+  double total = 0.0;
+  int c = 0;
+  n = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    n += s_n[w];
+    if (tid < lanes * 4) {
+      total += s_sum[w][tid];
+      c += s_count[w][tid];
+    }
+  }
+  const int e = first + tid;
+  double term = 0.0;
+  if (tid < lanes * 4 && e < E) {
+    const double p = n > 0 ? total / n : 0.0;
+    counts[(size_t)g * E + e] = c;
+    probs[(size_t)g * E + e] = (float)p;
+    term = (double)c * p;
+  }
+#pragma unroll
+  for (int off = kPieceLanes * 2; off > 0; off >>= 1) term += __shfl_xor(term, off);
+  if (tid != 0) return;
+  if (pieces > 1) {
+    double* const terms = partial.terms + (size_t)g * kMaxPieces;
+    __hip_atomic_store(terms + piece, term, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (__hip_atomic_fetch_add(partial.done + g, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) != (unsigned)pieces - 1) return;
+    term = 0.0;
+    for (int i = 0; i < pieces; ++i) term += __hip_atomic_load(terms + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  n_tokens[g] = n;
+  loss[g] = n > 0 ? (float)(term * E / ((double)k * n)) : 0.f;
 }
 
 struct BackwardArgs {
@@ -384,8 +434,7 @@ template <typename Fn> void with_lanes(int E, Fn&& fn) {
   else fn(std::integral_constant<int, 64>{});
 }
 
-constexpr int kParts = 256;       // workgroups that share the tokens of a batch in balance_kernel, about
-constexpr int kBackParts = 2048;  // ... and in route_backward_kernel, which leaves no sums to be added
+constexpr int kBackParts = 2048;  // workgroups that share the tokens of a batch in route_backward_kernel, which leaves no sums to be added
 constexpr int kMaxGroups = PRISM_MAX_BALANCE_GROUPS;   // (a workgroup each: below 2^32 threads)
 
 // The groups of a batch, and how many workgroups share one: at least one pass of rows each, and one workgroup for up to
@@ -405,7 +454,7 @@ bool aligned16(const void* a, const void* b) { return (((uintptr_t)a | (uintptr_
 
 }  // namespace
 
-size_t balance_workspace_bytes(int E) { return align_up((size_t)kParts * (2 * align_up(E, 4) + 1) * 4, 256); }
+size_t balance_workspace_bytes(int E) { return align_up(partial_bytes(E), 256); }
 
 prism_status launch_balance(const prism_layer_desc& d, const float* logits, const int32_t* topk_idx, const uint8_t* mask,
                             int group_tokens, int T, float* loss, int32_t* counts, float* probs, int32_t* n_tokens,
@@ -420,12 +469,15 @@ prism_status launch_balance(const prism_layer_desc& d, const float* logits, cons
       status = PRISM_ERR_UNSUPPORTED;
       return;
     }
-    const Partial partial = partial_of(workspace, G * a.parts, a.E);
+    const Partial partial = partial_of(workspace, a.E);
     hipLaunchKernelGGL((balance_kernel<LPR>), dim3((unsigned)G * a.parts), dim3(kThreads), 0, st, a, partial, counts, probs, n_tokens,
                        loss);
-    if (a.parts > 1)
-      hipLaunchKernelGGL(finish_kernel, dim3((unsigned)G), dim3(kFinishThreads), 0, st, partial, a.E, a.k, a.parts, LPR, counts, probs,
-                         n_tokens, loss);
+    if (a.parts > 1) {
+      constexpr int kLanes = std::min(LPR, kPieceLanes);
+      const int pieces = ceil_div(a.E, 4 * kLanes);
+      hipLaunchKernelGGL(finish_kernel, dim3((unsigned)(G * pieces)), dim3(kFinishThreads), 0, st, partial, a.E, a.k, a.parts, kLanes,
+                         pieces, counts, probs, n_tokens, loss);
+    }
   });
   PRISM_TRY(status);
   PRISM_CHECK_LAUNCH();

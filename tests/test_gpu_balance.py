@@ -76,6 +76,23 @@ def test_sizes_and_groups(T, E, k, group, masked):
     _check(E, k, group, "renormalized", *_inputs(T, E, k, group, masked, T + E))
 
 
+def test_groups_that_several_workgroups_share():
+    """Their sums are made by several and added by several, on one workspace, whatever it holds."""
+    cases = [(3000, 200, 5, 700), (6000, 67, 3, 2500), (9001, 40, 6, 0), (2501, 256, 8, 1250)]
+    ws = P.alloc_balance_workspace(P.make_desc(64, 64, 256, 8))
+    for T, E, k, group in cases:
+        inputs = _inputs(T, E, k, group, True, T)
+        _check(E, k, group, "renormalized", *inputs)
+        desc = P.make_desc(64, 64, E, k)
+        logits, idx, mask = (_dev(a) for a in inputs[:3])
+        first = P.prism_balance_loss(desc, logits, idx, ws, mask, group)
+        for fill in (255, 0, 255):
+            ws.fill_(fill)
+            again = P.prism_balance_loss(desc, logits, idx, ws, mask, group)
+            for name in ("loss", "counts", "probs", "n_tokens"):
+                assert torch.equal(getattr(first, name), getattr(again, name)), name
+
+
 @pytest.mark.parametrize("E", [8, 64, 256])
 def test_addresses_that_are_not_16_byte_aligned(E):
     for offset in (1, 2, 3):
