@@ -190,7 +190,8 @@ prism_status prism_route(const prism_layer_desc* desc, const void* x, const void
  *   loss[g]     = E / (k n_tokens[g]) * sum_e counts[g,e] probs[g,e]              [G] fp32
  *                 (1 for an even spread; all of these are 0 for a group without tokens)
  * Sums over tokens run in an order that depends on the sizes alone.  The workspace (256-byte aligned, at least
- * prism_balance_workspace_bytes, which depends on E alone) holds partial sums during the call.
+ * prism_balance_workspace_bytes, which depends on E alone) holds partial sums during the call: not for two calls that may
+ * overlap in time.
  */
 #define PRISM_MAX_BALANCE_GROUPS (1 << 23)
 prism_status prism_balance_workspace_bytes(const prism_layer_desc* desc, size_t* bytes);
@@ -402,20 +403,22 @@ prism_status prism_pack_weights(const void* src, int32_t rows, int32_t cols, voi
  * 8-bit matrices (see PRISM_WEIGHTS_INT8 above) and their product.
  *
  * prism_quantize_i8: rows of a matrix in 8 bits -- activations with a scale per token, or weights with one per output channel.
- *   scale[r] = max |src[r]| * (1 / 127), both factors and the product in fp32;  byte = the integer nearest to src[r,c] / scale[r], exactly, ties to even, at
- *   most 127 in magnitude.  A row of zeros has scale 0, one with a NaN or an infinity such a scale (and zeros).
+ *   scale[r] = max |src[r]| * (1 / 127), both factors and the product in fp32
+ *   byte     = the integer nearest to src[r,c] / scale[r], exactly, ties to even, at most 127 in magnitude
+ *   A row of zeros has scale 0, one with a NaN or an infinity such a scale (and zeros).
  *   src  [rows, cols] of prism_dtype src_dtype, ld elements from row to row; aligned to its elements
  * prism_pack_i8: the same from bytes and scales that exist already (bytes are taken as they are, -128 too).
  *   src  [rows, cols], ld bytes from row to row;  scale [rows]
  * prism_matmul_i8: out[i,j] = (sum over l < k of a[i,l] b[j,l]) * scale_a[i] * scale_b[j], the sum exact, one rounding
- *   at each product and one to out_dtype.  (Contractions that the library shares among workgroups: the fp32 values of up to 8 parts are added
- *   in their order.)
+ *   at each product and one to out_dtype.  (Contractions that the library shares among workgroups: the fp32 values of
+ *   up to 8 parts are added in their order.)
  *   a  [m,k], b [n,k] 8-bit matrices;  out [m,n] of prism_dtype out_dtype, ldo elements from row to row, of which only
  *   the first n are written
  *   workspace  256-byte aligned, prism_matmul_i8_workspace_bytes(max_m, n, k) for every m <= max_m; not for two calls
  *   that may overlap in time
- * Errors: INVALID_ARG (NULL, misaligned, sizes < 1, a row longer than ld), UNSUPPORTED (more than 130944 columns; a or b of 4 GiB or
- * more in a product), WORKSPACE_TOO_SMALL.  No rows (m or rows of prism_quantize_i8 0) is PRISM_OK, with nothing launched.
+ * Errors: INVALID_ARG (NULL, misaligned, sizes < 1, a row longer than ld), UNSUPPORTED (more than 130944 columns; a or
+ * b of 4 GiB or more in a product), WORKSPACE_TOO_SMALL.  No rows (m or rows of prism_quantize_i8 0) is PRISM_OK, with
+ * nothing launched.
  */
 prism_status prism_i8_bytes(int32_t rows, int32_t cols, size_t* bytes);
 prism_status prism_quantize_i8(const void* src, int32_t src_dtype, int64_t ld, int32_t rows, int32_t cols, void* dst,

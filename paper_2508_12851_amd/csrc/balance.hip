@@ -434,7 +434,7 @@ template <typename Fn> void with_lanes(int E, Fn&& fn) {
   else fn(std::integral_constant<int, 64>{});
 }
 
-constexpr int kBackParts = 2048;  // workgroups that share the tokens of a batch in route_backward_kernel, which leaves no sums to be added
+constexpr int kBackParts = 2048;  // of route_backward_kernel, about: it leaves no sums to be added
 constexpr int kMaxGroups = PRISM_MAX_BALANCE_GROUPS;   // (a workgroup each: below 2^32 threads)
 
 // The groups of a batch, and how many workgroups share one: at least one pass of rows each, and one workgroup for up to

@@ -85,8 +85,8 @@ enum class FfnPath {
   kPrefillShort    // the same with a short ring
 };
 
-// The path of a batch of T > 0 tokens of layer d (bf16 layers; the figures are those of bf16 weights.  8-bit ones, FFN of 25 batches of 70 to
-// 2500 tokens in every path that can take them: the path chosen was the fastest or within 4 % of it).
+// The path of a batch of T > 0 tokens of layer d (bf16 layers; the figures are those of bf16 weights.  8-bit ones, FFN of 25
+// batches of 70 to 2500 tokens in every path that can take them: the path chosen was the fastest or within 4 % of it).
 static inline FfnPath ffn_path(const prism_layer_desc& d, int T) {
   const int k1 = contraction(d, d.hidden), k2 = contraction(d, d.ffn);
   if (T <= kDecodeMaxTokens) {

@@ -21,12 +21,12 @@ struct Plan {
 };
 
 // The tile and the splits of a product, by an estimate of its time in us.  A round of items takes a fixed time and so much
-// per k-tile of 128 bytes, more as more workgroups share the L2: fitted to 20 products from 1 x 1024 x 4096 to 4096 x 4096 x 14336, weights
-// from HBM, of which each was run with all tiles and 1 to 8 splits.  Two 64 x 64 items share a CU, each then 1.5 times as long.
-// A split costs the kernel that adds the parts and their traffic; more workgroups than CUs by splits were slower everywhere.
-// Measured, us, 64 x 64 / 64 x 128 / 128 x 128 (best number of splits of each): 1 x 4096 x 14336 16.9 / 18.0; 64 x 14336 x 4096
-// 15.8 / 20.2; 128 x 14336 x 4096 23.7 / 19.8 / 23.9; 300 x 11008 x 4096 34.2 / 28.2 / 33.5; 600 x 4096 x 8192 59.5 / 49.5 / 36.5; 1000 x 4096 x
-// 4096 32.8 / 28.2 / 22.1 (256 x 256 39.7); 2000 x 4096 x 4096 64.1 / 52.0 / 40.0 (45.8).
+// per k-tile of 128 bytes, more as more workgroups share the L2: fitted to 20 products from 1 x 1024 x 4096 to 4096 x 4096 x
+// 14336, weights from HBM, of which each was run with all tiles and 1 to 8 splits.  Two 64 x 64 items share a CU, each then 1.5
+// times as long.  A split costs the kernel that adds the parts and their traffic; more workgroups than CUs by splits were
+// slower everywhere.  Measured, us, 64 x 64 / 64 x 128 / 128 x 128 (best number of splits of each): 1 x 4096 x 14336 16.9 / 18.0;
+// 64 x 14336 x 4096 15.8 / 20.2; 128 x 14336 x 4096 23.7 / 19.8 / 23.9; 300 x 11008 x 4096 34.2 / 28.2 / 33.5; 600 x 4096 x 8192
+// 59.5 / 49.5 / 36.5; 1000 x 4096 x 4096 32.8 / 28.2 / 22.1 (256 x 256 39.7); 2000 x 4096 x 4096 64.1 / 52.0 / 40.0 (45.8).
 struct TileCost {
   Tile tile;
   int bm, bn, resident;     // resident: workgroups of a CU

@@ -227,7 +227,7 @@ __global__ __launch_bounds__(kThreads) void pack_i8_kernel(const int8_t* __restr
         v = *reinterpret_cast<const uint4*>(row + c);
       } else {
         uint32_t w[4] = {0u, 0u, 0u, 0u};
-  #pragma unroll
+#pragma unroll
         for (int i = 0; i < 16; ++i)
           if (c + i < cols) w[i / 4] |= (uint32_t)(uint8_t)row[c + i] << (8 * (i % 4));
         v = uint4{w[0], w[1], w[2], w[3]};
@@ -300,8 +300,8 @@ prism_status launch_quantize_tokens(const prism_layer_desc& d, const QuantizeArg
 
 prism_status launch_pack_i8(const int8_t* src, long long ld, const float* scale, int rows, int cols, void* dst, hipStream_t st) {
   const int vec = ((uintptr_t)src & 15u) == 0 && ld % 16 == 0;
-  hipLaunchKernelGGL(pack_i8_kernel, dim3((unsigned)std::min(rows, kMaxGrid)), dim3(kThreads), 0, st, src, ld, scale, rows, cols, vec, (uint8_t*)dst,
-                     (float*)((uint8_t*)dst + i8_elements(rows, cols)));
+  hipLaunchKernelGGL(pack_i8_kernel, dim3((unsigned)std::min(rows, kMaxGrid)), dim3(kThreads), 0, st, src, ld, scale, rows, cols,
+                     vec, (uint8_t*)dst, (float*)((uint8_t*)dst + i8_elements(rows, cols)));
   PRISM_CHECK_LAUNCH();
   return PRISM_OK;
 }
