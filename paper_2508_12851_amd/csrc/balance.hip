@@ -32,7 +32,6 @@ struct RowArgs {
   int T, E, k;
   int group;                  // tokens of a group
   int parts, part_rows;       // workgroups of a group and the tokens of each
-  bool vec;                   // rows can be moved 16 bytes at a time
 };
 
 // Tokens [first, end) of this workgroup: part blockIdx.x % parts of group blockIdx.x / parts.
@@ -73,8 +72,8 @@ template <int LPR> constexpr int back_ahead_of = LPR >= 16 ? 2 : 1;
 __device__ __forceinline__ f32x4 load_row(const RowArgs& a, int row, int e0) {
   const float* p = a.logits + (size_t)row * a.E + e0;
   f32x4 v = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-  if (a.vec) {
-    if (e0 < a.E) v = *reinterpret_cast<const f32x4*>(p);
+  if (e0 + 4 <= a.E) {
+    v = reinterpret_cast<const Unaligned<f32x4, 4>*>(p)->v;
   } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -411,8 +410,8 @@ __global__ __launch_bounds__(kBackThreads) void route_backward_kernel(const Back
       const int row = row0 + s * kRows + lane / LPR;
       if (row < r.end) {
         float* out = b.d_logits + (size_t)row * a.E + e0;
-        if (a.vec) {
-          if (e0 < a.E) *reinterpret_cast<f32x4*>(out) = d;
+        if (e0 + 4 <= a.E) {
+          reinterpret_cast<Unaligned<f32x4, 4>*>(out)->v = d;
         } else {
 #pragma unroll
           for (int i = 0; i < 4; ++i)
@@ -450,8 +449,6 @@ int split_groups(RowArgs* a, int group_tokens, int T, int most, int rows_per_pas
   return G;
 }
 
-bool aligned16(const void* a, const void* b) { return (((uintptr_t)a | (uintptr_t)b) & 15u) == 0; }
-
 }  // namespace
 
 size_t balance_workspace_bytes(int E) { return align_up(partial_bytes(E), 256); }
@@ -460,7 +457,7 @@ prism_status launch_balance(const prism_layer_desc& d, const float* logits, cons
                             int group_tokens, int T, float* loss, int32_t* counts, float* probs, int32_t* n_tokens,
                             void* workspace, hipStream_t st) {
   if (T == 0 && group_tokens > 0) return PRISM_OK;    // no groups
-  RowArgs a{logits, topk_idx, mask, T, d.n_experts, d.top_k, 0, 1, 0, d.n_experts % 4 == 0 && aligned16(logits, nullptr)};
+  RowArgs a{logits, topk_idx, mask, T, d.n_experts, d.top_k, 0, 1, 0};
   prism_status status = PRISM_OK;
   with_lanes(a.E, [&](auto lanes) {
     constexpr int LPR = decltype(lanes)::value;
@@ -488,8 +485,7 @@ prism_status launch_route_backward(const prism_layer_desc& d, const float* logit
                                    int group_tokens, int T, const int32_t* counts, const int32_t* n_tokens, const float* d_loss,
                                    const float* d_gate, float* d_logits, hipStream_t st) {
   if (T == 0) return PRISM_OK;
-  BackwardArgs b{{logits, topk_idx, mask, T, d.n_experts, d.top_k, 0, 1, 0, d.n_experts % 4 == 0 && aligned16(logits, d_logits)},
-                 d_gate, counts, n_tokens, d_loss, d_logits, d.gate_mode == PRISM_GATES_SOFTMAX_ALL};
+  BackwardArgs b{{logits, topk_idx, mask, T, d.n_experts, d.top_k, 0, 1, 0}, d_gate, counts, n_tokens, d_loss, d_logits, d.gate_mode == PRISM_GATES_SOFTMAX_ALL};
   prism_status status = PRISM_OK;
   with_lanes(b.r.E, [&](auto lanes) {
     constexpr int LPR = decltype(lanes)::value;

@@ -82,7 +82,6 @@ struct GemmArgs {
   void* dense_out;          // [c_rows, N] with dense_ldo elements from row to row
   long long dense_ldo;
   int dense_f32;            // fp32 instead of bf16
-  int dense_vec;            // 1: rows can be stored 4 elements at a time; 2: bf16, 8 elements
   int dense_splits;         // SPLITK: workgroups that share an item
 };
 
@@ -113,7 +112,6 @@ template <int WN, bool GATED, bool SPLITK> constexpr bool staged_store() {
   return !SPLITK && !GATED && (WN / 32) % 2 == 0;
 }
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef int32_t i32x16 __attribute__((ext_vector_type(16)));
 
@@ -158,11 +156,11 @@ constexpr int gemm_lds_bytes() {
   return gemm_lds_unstaged<BM, BN, WGN, BK, STAGES, GATED, I8>() + (staged ? 4 * kStripBytes : 0);   // + strips
 }
 // Elements n .. n + 3 of a row of a dense product with N columns.
-__device__ __forceinline__ void store_dense(void* out, long long ldo, int f32, int vec, size_t row, int n, int N, const f32x4& v) {
+__device__ __forceinline__ void store_dense(void* out, long long ldo, int f32, size_t row, int n, int N, const f32x4& v) {
   if (f32) {
     float* const p = (float*)out + row * (size_t)ldo + n;
-    if (vec && n + 4 <= N) {
-      *reinterpret_cast<f32x4*>(p) = v;
+    if (n + 4 <= N) {
+      reinterpret_cast<Unaligned<f32x4, 4>*>(p)->v = v;
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
@@ -170,8 +168,8 @@ __device__ __forceinline__ void store_dense(void* out, long long ldo, int f32, i
     }
   } else {
     bf16_t* const p = (bf16_t*)out + row * (size_t)ldo + n;
-    if (vec && n + 4 <= N) {
-      *reinterpret_cast<bf16x4*>(p) = bf16x4{(bf16_t)v[0], (bf16_t)v[1], (bf16_t)v[2], (bf16_t)v[3]};
+    if (n + 4 <= N) {
+      reinterpret_cast<Unaligned<bf16x4, 2>*>(p)->v = bf16x4{(bf16_t)v[0], (bf16_t)v[1], (bf16_t)v[2], (bf16_t)v[3]};
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e)

@@ -518,7 +518,7 @@
           } else if constexpr (SPLITK) {
             *reinterpret_cast<f32x4*>(p.Cpart + ((size_t)split * p.c_rows + crow) * (DENSE ? (p.N + 3) / 4 * 4 : p.N) + n) = o;
           } else if constexpr (DENSE) {
-            store_dense(p.dense_out, p.dense_ldo, p.dense_f32, p.dense_vec, crow, n, p.N, o);
+            store_dense(p.dense_out, p.dense_ldo, p.dense_f32, crow, n, p.N, o);
           } else {
             *reinterpret_cast<bf16x4*>(p.C + crow * p.N + n) =
                 bf16x4{(bf16_t)o[0], (bf16_t)o[1], (bf16_t)o[2], (bf16_t)o[3]};
@@ -571,8 +571,16 @@
           const int row = row0 + t * 8 + rd_row;
           if (row >= cx.row_count || col >= p.N) continue;
           const size_t crow = (size_t)(cx.row_start + row);
-          if constexpr (DENSE) *reinterpret_cast<u32x4*>((uint16_t*)p.dense_out + crow * (size_t)p.dense_ldo + col) = v[t];
-          else *reinterpret_cast<u32x4*>(p.C + crow * p.N + col) = v[t];
+          if constexpr (DENSE) {
+            uint16_t* const out = (uint16_t*)p.dense_out + crow * (size_t)p.dense_ldo + col;
+            if (col + 8 <= p.N) {
+              reinterpret_cast<Unaligned<u32x4, 2>*>(out)->v = v[t];
+            } else {
+#pragma unroll
+              for (int e = 0; e < 7; ++e)
+                if (col + e < p.N) out[e] = (uint16_t)(v[t][e / 2] >> (e % 2 * 16));
+            }
+          } else *reinterpret_cast<u32x4*>(p.C + crow * p.N + col) = v[t];
         }
       }
     }
@@ -580,7 +588,7 @@
   auto epilogue = [&](const Ctx& cx, int parity) {
     if constexpr (I8) {
       if constexpr (!kStagedStore) epilogue_i8(cx, parity);
-      else if (!DENSE || p.dense_vec == 2) epilogue_i8_staged(cx, parity);
+      else if (!DENSE || !p.dense_f32) epilogue_i8_staged(cx, parity);
       else epilogue_i8(cx, parity);
     } else {
       if constexpr (SLICES) {

@@ -67,7 +67,7 @@ Plan plan_of(int M, int N, int K) {
 
 // out = sum of the splits' partial sums, in their order: four columns per thread.
 __global__ __launch_bounds__(256) void reduce_dense_kernel(const float* __restrict__ part, int splits, int M, int N, void* out,
-                                                           long long ldo, int f32, int vec) {
+                                                           long long ldo, int f32) {
   const int pitch = (N + 3) / 4 * 4, quads = pitch / 4;
   const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
   if (i >= (long long)M * quads) return;
@@ -80,7 +80,7 @@ __global__ __launch_bounds__(256) void reduce_dense_kernel(const float* __restri
 #pragma unroll
   for (int s = 0; s < kMaxSplits; ++s)
     if (s < splits) sum += v[s];
-  gg::store_dense(out, ldo, f32, vec, row, n, N, sum);
+  gg::store_dense(out, ldo, f32, row, n, N, sum);
 }
 
 template <int BM, int BN, int BK, int STAGES, bool CAN_SPLIT>
@@ -124,9 +124,6 @@ prism_status launch_matmul_i8(const void* a, const void* b, int M, int N, int K,
   g.dense_out = out;
   g.dense_ldo = ldo;
   g.dense_f32 = out_dtype == PRISM_F32;
-  const int es = g.dense_f32 ? 4 : 2;
-  g.dense_vec = ((uintptr_t)out & (4 * es - 1)) == 0 && ldo % 4 == 0;
-  if (!g.dense_f32 && ((uintptr_t)out & 15) == 0 && ldo % 8 == 0 && N % 8 == 0) g.dense_vec = 2;
   g.dense_splits = plan.splits;
   switch (plan.tile) {
     case Tile::k64x64: PRISM_TRY((launch_tiles<64, 64, 64, 4, true>(g, st))); break;
@@ -138,7 +135,7 @@ prism_status launch_matmul_i8(const void* a, const void* b, int M, int N, int K,
   if (plan.splits > 1) {
     const long long threads = (long long)M * (align_up(N, 4) / 4);
     hipLaunchKernelGGL(reduce_dense_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, (const float*)workspace,
-                       plan.splits, M, N, out, ldo, g.dense_f32, g.dense_vec);
+                       plan.splits, M, N, out, ldo, g.dense_f32);
     PRISM_CHECK_LAUNCH();
   }
   return PRISM_OK;

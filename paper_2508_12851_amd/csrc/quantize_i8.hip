@@ -30,8 +30,8 @@ template <> struct Chunk<float> {
   typedef uint32_t Max;
   f32x4 a, b;
   __device__ void load(const float* p) {
-    a = reinterpret_cast<const f32x4*>(p)[0];
-    b = reinterpret_cast<const f32x4*>(p)[1];
+    a = reinterpret_cast<const Unaligned<f32x4, 4>*>(p)[0].v;
+    b = reinterpret_cast<const Unaligned<f32x4, 4>*>(p)[1].v;
   }
   __device__ void set(int i, float v) { (i < 4 ? a : b)[i & 3] = v; }
   __device__ __forceinline__ float get(int i) const { return (i < 4 ? a : b)[i & 3]; }
@@ -43,29 +43,27 @@ template <> struct Chunk<float> {
 };
 template <> struct Chunk<bf16_t> {
   typedef u16x2 Max;
-  uint4 a;
-  __device__ void load(const bf16_t* p) { a = *reinterpret_cast<const uint4*>(p); }
+  u32x4 a;
+  __device__ void load(const bf16_t* p) { a = reinterpret_cast<const Unaligned<u32x4, 2>*>(p)->v; }
   __device__ void set(int i, bf16_t v) {
-    uint32_t& w = i < 2 ? a.x : i < 4 ? a.y : i < 6 ? a.z : a.w;
-    const uint32_t b = __builtin_bit_cast(uint16_t, v);
-    w = i & 1 ? (w & 0xffffu) | b << 16 : (w & 0xffff0000u) | b;
+    const uint32_t w = a[i / 2], b = __builtin_bit_cast(uint16_t, v);
+    a[i / 2] = i & 1 ? (w & 0xffffu) | b << 16 : (w & 0xffff0000u) | b;
   }
   __device__ __forceinline__ float get(int i) const {
-    const uint32_t w = i < 2 ? a.x : i < 4 ? a.y : i < 6 ? a.z : a.w;
+    const uint32_t w = a[i / 2];
     return i & 1 ? bf16_hi(w) : bf16_lo(w);
   }
   __device__ __forceinline__ void grow(Max& m) const {
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w[i] & 0x7fff7fffu));
+    for (int i = 0; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, a[i] & 0x7fff7fffu));
   }
   static __device__ __forceinline__ uint32_t bits_of(Max m) { return (uint32_t)max(m.x, m.y) << 16; }
 };
 
 // Elements c .. c + 7 of a row of n, zeros past its end.
-template <typename S, bool VEC> __device__ __forceinline__ Chunk<S> load_chunk(const S* row, int c, int n) {
+template <typename S> __device__ __forceinline__ Chunk<S> load_chunk(const S* row, int c, int n) {
   Chunk<S> v{};
-  if (VEC && c + kElems <= n) {
+  if (c + kElems <= n) {
     v.load(row + c);
   } else {
 #pragma unroll
@@ -123,7 +121,7 @@ __device__ __forceinline__ size_t byte_of(int r, int c, size_t row_bytes, bool t
 }
 
 // Row r on LANES lanes (a wavefront, or a workgroup), `lane` of them this one.
-template <typename S, bool VEC, int LANES, int HELD>
+template <typename S, int LANES, int HELD>
 __device__ __forceinline__ void quantize_row(const QuantizeArgs& a, int r, int lane) {
   int from = r;
   if (a.local_offsets != nullptr) {
@@ -138,11 +136,11 @@ __device__ __forceinline__ void quantize_row(const QuantizeArgs& a, int r, int l
   typename Chunk<S>::Max grown{};
 #pragma unroll
   for (int i = 0; i < HELD; ++i)
-    if (c0 + i * kPass < a.cols) held[i] = load_chunk<S, VEC>(row, c0 + i * kPass, a.cols);
+    if (c0 + i * kPass < a.cols) held[i] = load_chunk<S>(row, c0 + i * kPass, a.cols);
 #pragma unroll
   for (int i = 0; i < HELD; ++i)
     if (c0 + i * kPass < a.cols) held[i].grow(grown);
-  for (int c = c0 + HELD * kPass; c < a.cols; c += kPass) load_chunk<S, VEC>(row, c, a.cols).grow(grown);
+  for (int c = c0 + HELD * kPass; c < a.cols; c += kPass) load_chunk<S>(row, c, a.cols).grow(grown);
   uint32_t m = Chunk<S>::bits_of(grown);
   m = max(m, (uint32_t)row_xor<1>((int)m));
   m = max(m, (uint32_t)row_xor<2>((int)m));
@@ -173,7 +171,7 @@ __device__ __forceinline__ void quantize_row(const QuantizeArgs& a, int r, int l
 #pragma unroll
   for (int i = 0; i < HELD; ++i)
     if (c0 + i * kPass < row_bytes) store(c0 + i * kPass, held[i]);
-  for (int c = c0 + HELD * kPass; c < row_bytes; c += kPass) store(c, load_chunk<S, VEC>(row, c, a.cols));
+  for (int c = c0 + HELD * kPass; c < row_bytes; c += kPass) store(c, load_chunk<S>(row, c, a.cols));
 }
 
 // The 16 rows of a tile belong to workgroups that the hardware deals to one XCD (workgroups 8 apart), whose L2 joins their 64-byte
@@ -182,22 +180,22 @@ __device__ __forceinline__ int same_xcd(int wg, int per, int wgs) {
   const int first = wg / (8 * per) * (8 * per), i = wg - first;
   return first + 8 * per <= wgs ? first + i % 8 * per + i / 8 : wg;
 }
-template <typename S, bool VEC, int LANES, int HELD>
+template <typename S, int LANES, int HELD>
 __device__ __forceinline__ void quantize_rows(const QuantizeArgs& a, int wg, int wgs) {
   if constexpr (LANES == 64) {
     const int all = (a.rows + 3) / 4;
     for (int w = wg; w < all; w += wgs) {
       const int r = same_xcd(w, 4, all) * 4 + (threadIdx.x >> 6);
-      if (r < a.rows) quantize_row<S, VEC, 64, HELD>(a, r, threadIdx.x & 63);
+      if (r < a.rows) quantize_row<S, 64, HELD>(a, r, threadIdx.x & 63);
     }
   } else {
-    for (int w = wg; w < a.rows; w += wgs) quantize_row<S, VEC, LANES, HELD>(a, same_xcd(w, 16, a.rows), threadIdx.x);
+    for (int w = wg; w < a.rows; w += wgs) quantize_row<S, LANES, HELD>(a, same_xcd(w, 16, a.rows), threadIdx.x);
   }
 }
 
-template <typename S, bool VEC, int LANES, int HELD>
+template <typename S, int LANES, int HELD>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void quantize_kernel(const QuantizeArgs a) {
-  quantize_rows<S, VEC, LANES, HELD>(a, blockIdx.x, gridDim.x);
+  quantize_rows<S, LANES, HELD>(a, blockIdx.x, gridDim.x);
 }
 
 // The tokens of an expert FFN, and the schedules of its two products: some workgroups more, where a launch of their own took 4 to 10 us.
@@ -210,29 +208,27 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void quantize_and_schedu
     const gg::sched_params_t<WIDTHS> p[1] = {blockIdx.x < kScheduleParts ? p0 : p1};
     gg::build_schedules_block<1, WIDTHS>(local_offsets, E, S, T, A_total, p, blockIdx.x % kScheduleParts, kScheduleParts);
   } else {
-    quantize_rows<bf16_t, true, LANES, HELD>(a, blockIdx.x - 2 * kScheduleParts, gridDim.x - 2 * kScheduleParts);
+    quantize_rows<bf16_t, LANES, HELD>(a, blockIdx.x - 2 * kScheduleParts, gridDim.x - 2 * kScheduleParts);
   }
 }
 
 // Rows of bytes that are quantised already, into tiles: a row per workgroup.
 __global__ __launch_bounds__(kThreads) void pack_i8_kernel(const int8_t* __restrict__ src, long long ld, const float* __restrict__ scale,
-                                                           int rows, int cols, int vec, uint8_t* __restrict__ dst,
+                                                           int rows, int cols, uint8_t* __restrict__ dst,
                                                            float* __restrict__ dst_scale) {
   const int row_bytes = (cols + kI8RowAlign - 1) / kI8RowAlign * kI8RowAlign;
   for (int r = blockIdx.x; r < rows; r += gridDim.x) {
     const int8_t* row = src + (size_t)r * ld;
     for (int c = threadIdx.x * 16; c < row_bytes; c += kThreads * 16) {
-      uint4 v{0u, 0u, 0u, 0u};
-      if (vec && c + 16 <= cols) {
-        v = *reinterpret_cast<const uint4*>(row + c);
+      u32x4 v = {0u, 0u, 0u, 0u};
+      if (c + 16 <= cols) {
+        v = reinterpret_cast<const Unaligned<u32x4, 1>*>(row + c)->v;
       } else {
-        uint32_t w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          if (c + i < cols) w[i / 4] |= (uint32_t)(uint8_t)row[c + i] << (8 * (i % 4));
-        v = uint4{w[0], w[1], w[2], w[3]};
+          if (c + i < cols) v[i / 4] |= (uint32_t)(uint8_t)row[c + i] << (8 * (i % 4));
       }
-      *reinterpret_cast<uint4*>(dst + byte_of(r, c, row_bytes, true)) = v;
+      *reinterpret_cast<u32x4*>(dst + byte_of(r, c, row_bytes, true)) = v;
     }
     if (threadIdx.x == 0) dst_scale[r] = scale[r];
   }
@@ -253,9 +249,6 @@ template <typename Fn> void with_row_lanes(const QuantizeArgs& a, Fn&& launch) {
   else if (a.rows > 512) launch(integral_constant<int, 512>{}, integral_constant<int, 4>{});
   else launch(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
 }
-template <typename S> bool rows_aligned(const QuantizeArgs& a) {
-  return ((uintptr_t)a.src & 15u) == 0 && a.ld * (long long)sizeof(S) % 16 == 0;
-}
 unsigned workgroups(const QuantizeArgs& a, int lanes) { return (unsigned)std::min(ceil_div(a.rows, lanes == 64 ? 4 : 1), kMaxGrid); }
 }  // namespace
 
@@ -266,8 +259,7 @@ prism_status launch_quantize(const QuantizeArgs& a, int src_dtype, hipStream_t s
     with_row_lanes(a, [&](auto lanes, auto held) {
       constexpr int L = decltype(lanes)::value, N = decltype(held)::value;
       const dim3 grid(workgroups(a, L)), block(L < 256 ? 256 : L);
-      if (rows_aligned<S>(a)) hipLaunchKernelGGL((quantize_kernel<S, true, L, N>), grid, block, 0, st, a);
-      else hipLaunchKernelGGL((quantize_kernel<S, false, L, N>), grid, block, 0, st, a);
+      hipLaunchKernelGGL((quantize_kernel<S, L, N>), grid, block, 0, st, a);
     });
   };
   if (src_dtype == PRISM_F32) of_type(float{});
@@ -278,10 +270,6 @@ prism_status launch_quantize(const QuantizeArgs& a, int src_dtype, hipStream_t s
 
 prism_status launch_quantize_tokens(const prism_layer_desc& d, const QuantizeArgs& a, const int32_t* local_offsets, int T,
                                     int32_t* tiles, hipStream_t st) {
-  if (!rows_aligned<bf16_t>(a)) {     // (prism.h asks for aligned tokens)
-    PRISM_TRY(launch_quantize(a, PRISM_BF16, st));
-    return gg::launch_build_schedules(d, local_offsets, T, tiles, st);
-  }
   gg::WidthParams p0, p1;
   gg::ffn_sched_params(d, T, tiles, &p0, &p1);
   with_row_lanes(a, [&](auto lanes, auto held) {
@@ -299,9 +287,8 @@ prism_status launch_quantize_tokens(const prism_layer_desc& d, const QuantizeArg
 }
 
 prism_status launch_pack_i8(const int8_t* src, long long ld, const float* scale, int rows, int cols, void* dst, hipStream_t st) {
-  const int vec = ((uintptr_t)src & 15u) == 0 && ld % 16 == 0;
   hipLaunchKernelGGL(pack_i8_kernel, dim3((unsigned)std::min(rows, kMaxGrid)), dim3(kThreads), 0, st, src, ld, scale, rows, cols,
-                     vec, (uint8_t*)dst, (float*)((uint8_t*)dst + i8_elements(rows, cols)));
+                     (uint8_t*)dst, (float*)((uint8_t*)dst + i8_elements(rows, cols)));
   PRISM_CHECK_LAUNCH();
   return PRISM_OK;
 }
