@@ -238,18 +238,21 @@ def prism_balance_loss(desc: LayerDesc, logits, topk_idx, workspace, token_mask=
     T, E, k = logits.shape[0], desc.n_experts, desc.top_k
     G = _balance_groups(T, group_tokens)
     f32, i32 = torch.float32, torch.int32
+    dev = torch.cuda.current_device()
+    inputs = (_typed(logits, f32, (T, E), dev, "logits"), _typed(topk_idx, i32, (T, k), dev, "topk_idx"),
+              _typed(token_mask, torch.uint8, (T,), dev, "token_mask"))
     o = outputs
     if o is None:
         new = logits.new_empty
-        o = BalanceOut(new((G,), dtype=f32), new((G, E), dtype=i32), new((G, E), dtype=f32), new((G,), dtype=i32))
+        o = BalanceOut(new((G,)), new((G, E), dtype=i32), new((G, E)), new((G,), dtype=i32))
+        made = o.loss.data_ptr(), o.counts.data_ptr(), o.probs.data_ptr(), o.n_tokens.data_ptr()
+    else:
+        made = (_typed(o.loss, f32, (G,), dev, "loss"), _typed(o.counts, i32, (G, E), dev, "counts"),
+                _typed(o.probs, f32, (G, E), dev, "probs"), _typed(o.n_tokens, i32, (G,), dev, "n_tokens"))
     if G == 0:                  # no tokens, no groups: nothing to address
         return o
-    dev = torch.cuda.current_device()
     _check(load_library().prism_balance_loss(
-        ctypes.byref(desc), _typed(logits, f32, (T, E), dev, "logits"), _typed(topk_idx, i32, (T, k), dev, "topk_idx"),
-        _typed(token_mask, torch.uint8, (T,), dev, "token_mask"), group_tokens, T, _typed(o.loss, f32, (G,), dev, "loss"),
-        _typed(o.counts, i32, (G, E), dev, "counts"), _typed(o.probs, f32, (G, E), dev, "probs"),
-        _typed(o.n_tokens, i32, (G,), dev, "n_tokens"), _bytes_on(workspace, dev, "workspace"), workspace.numel(),
+        ctypes.byref(desc), *inputs, group_tokens, T, *made, _bytes_on(workspace, dev, "workspace"), workspace.numel(),
         _stream_on(dev, stream)), "prism_balance_loss")
     return o
 
@@ -263,18 +266,22 @@ def prism_route_backward(desc: LayerDesc, logits, topk_idx, balance: Optional[Ba
     f32, i32 = torch.float32, torch.int32
     if (balance is None) != (d_loss is None):
         raise PrismError("d_loss comes with the balance it is the gradient of")
+    dev = torch.cuda.current_device()
+    logits_ptr = _typed(logits, f32, (T, E), dev, "logits")
     if d_logits is None:
-        d_logits = logits.new_empty((T, E), dtype=f32)
+        d_logits = torch.empty_like(logits)
+        d_ptr = d_logits.data_ptr()
+    else:
+        d_ptr = _typed(d_logits, f32, (T, E), dev, "d_logits")
     if T == 0:
         return d_logits
-    dev = torch.cuda.current_device()
     _check(load_library().prism_route_backward(
-        ctypes.byref(desc), _typed(logits, f32, (T, E), dev, "logits"), _typed(topk_idx, i32, (T, k), dev, "topk_idx"),
+        ctypes.byref(desc), logits_ptr, _typed(topk_idx, i32, (T, k), dev, "topk_idx"),
         _typed(token_mask, torch.uint8, (T,), dev, "token_mask"), group_tokens, T,
         None if balance is None else _typed(balance.counts, i32, (G, E), dev, "counts"),
         None if balance is None else _typed(balance.n_tokens, i32, (G,), dev, "n_tokens"),
         _typed(d_loss, f32, (G,), dev, "d_loss"), _typed(d_gate, f32, (T, k), dev, "d_gate"),
-        _typed(d_logits, f32, (T, E), dev, "d_logits"), _stream_on(dev, stream)), "prism_route_backward")
+        d_ptr, _stream_on(dev, stream)), "prism_route_backward")
     return d_logits
 
 
@@ -590,13 +597,15 @@ def prism_matmul_i8(a: I8Matrix, b: I8Matrix, workspace, out=None, dtype=torch.b
     """a b^T of two 8-bit matrices [m, k] and [n, k]: [m, n] in bf16 or fp32."""
     if a.cols != b.cols:
         raise PrismError(f"rows of {a.cols} and of {b.cols} elements")
+    dev = torch.cuda.current_device()
     if out is None:
         out = b.data.new_empty((a.rows, b.rows), dtype=dtype)
-    elif out.shape != (a.rows, b.rows):
-        raise PrismError(f"out has to be {a.rows} x {b.rows}, not {tuple(out.shape)}")
-    dev = torch.cuda.current_device()
+        ptr, ldo = out.data_ptr(), b.rows
+    else:
+        if out.shape != (a.rows, b.rows):
+            raise PrismError(f"out has to be {a.rows} x {b.rows}, not {tuple(out.shape)}")
+        ptr, ldo = _rows_ptr(out, dev, "out")
     out_dtype = _float_dtype(out, "out")
-    ptr, ldo = _rows_ptr(out, dev, "out")
     _check(load_library().prism_matmul_i8(_bytes_on(a.data, dev, "a"), _bytes_on(b.data, dev, "b"), a.rows, b.rows, a.cols, ptr, ldo,
                                           out_dtype, _bytes_on(workspace, dev, "workspace"), workspace.numel(),
                                           _stream_on(dev, stream)), "prism_matmul_i8")

@@ -10,9 +10,9 @@
 //
 // Rows: a token's E logits lie on 2^n lanes with 4 consecutive experts each, so that a wavefront holds one row of 256
 // experts or 64 rows of 4, and row sums are exchanges between lanes.  Both passes read the logits once: 65531 tokens of 256
-// experts (67 MB) 20 us for the sums (3.4 TB/s) and 8 to add their 256 parts, 36 us for the gradient (3.7 TB/s in and out; a
-// large copy reaches 4.8): the vector ALU, about 100 and 210 instructions a row, takes nearly as long as memory.  Below a few MB the
-// launches' latency: 8192 tokens of 64 experts in 16 groups 10 + 5 us.
+// experts (67 MB) 17 us for the sums (3.9 TB/s) and 8 to add their 256 parts, 34 us for the gradient (3.9 TB/s in and out; a
+// large copy reaches 4.8): the vector ALU, about 100 and 210 instructions a row, takes nearly as long as memory.  Below a few MB
+// the launches' latency: 8192 tokens of 64 experts in 16 groups 9 + 5 us.
 #include <type_traits>
 
 #include "prism_internal.h"
@@ -97,7 +97,8 @@ template <int LPR> __device__ __forceinline__ void softmax_row(f32x4& v) {
 // A group's results from its sums: probs, loss and the counts.  sum_p of expert threadIdx.x, in 64 bits; all threads call it.
 __device__ __forceinline__ void finish_group(int g, int E, int k, int n, int count, double sum_p, int32_t* counts, float* probs,
                                              int32_t* n_tokens, float* loss) {
-  __shared__ double s_term[kMaxE];
+  constexpr int kWaves = kMaxE / 64;
+  __shared__ double s_term[kWaves];
   const int e = threadIdx.x;
   double term = 0.0;
   if (e < E) {
@@ -106,14 +107,16 @@ __device__ __forceinline__ void finish_group(int g, int E, int k, int n, int cou
     probs[(size_t)g * E + e] = (float)p;
     term = (double)count * p;
   }
-  if (e < kMaxE) s_term[e] = term;
-  for (int half = kMaxE / 2; half > 0; half >>= 1) {
-    __syncthreads();
-    if (e < half) s_term[e] += s_term[e + half];
-  }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) term += __shfl_xor(term, off);
+  if (e < kMaxE && (e & 63) == 0) s_term[e >> 6] = term;
+  __syncthreads();
   if (e == 0) {
+    term = 0.0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) term += s_term[w];
     n_tokens[g] = n;
-    loss[g] = n > 0 ? (float)(s_term[0] * E / ((double)k * n)) : 0.f;
+    loss[g] = n > 0 ? (float)(term * E / ((double)k * n)) : 0.f;
   }
 }
 
@@ -161,14 +164,17 @@ __global__ __launch_bounds__(kThreads) void balance_kernel(const RowArgs a, cons
   if (tid == 0) s_n = 0;
   __syncthreads();
   int live_rows = 0;
-  for (int row = r.first + tid; row < r.end; row += kThreads) live_rows += a.mask == nullptr || a.mask[row] != 0;
-  if (live_rows > 0) atomicAdd(&s_n, live_rows);
-  const long long picks = (long long)(r.end - r.first) * a.k;
-  for (long long i = tid; i < picks; i += kThreads) {
-    const int row = r.first + (int)(i / a.k);
-    const int e = a.topk_idx[(size_t)r.first * a.k + i];
-    if ((unsigned)e < (unsigned)a.E && (a.mask == nullptr || a.mask[row] != 0)) atomicAdd(&s_counts[e], 1);
+  for (int row = r.first + tid; row < r.end; row += kThreads) {
+    if (a.mask != nullptr && a.mask[row] == 0) continue;
+    ++live_rows;
+    int e[PRISM_MAX_TOPK];
+#pragma unroll
+    for (int j = 0; j < PRISM_MAX_TOPK; ++j) e[j] = j < a.k ? a.topk_idx[(size_t)row * a.k + j] : -1;
+#pragma unroll
+    for (int j = 0; j < PRISM_MAX_TOPK; ++j)
+      if ((unsigned)e[j] < (unsigned)a.E) atomicAdd(&s_counts[e[j]], 1);
   }
+  if (live_rows > 0) atomicAdd(&s_n, live_rows);
   const int e0 = (lane % LPR) * 4;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
   for (int row0 = r.first + wave * kRows * kAhead; row0 < r.end; row0 += kWaves * kRows * kAhead) {
