@@ -125,6 +125,18 @@ def _stream_on(dev: int, stream: Optional[torch.cuda.Stream]) -> Optional[int]:
     return (torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream) or None
 
 
+def _new_on(stream: Optional[torch.cuda.Stream], like: torch.Tensor):
+    """like.new_empty for the outputs of a call on `stream`: of that stream's memory.  What the current stream has freed, it may
+    still have to read."""
+    if stream is None:
+        return like.new_empty
+
+    def new(shape, dtype=None):
+        with torch.cuda.stream(stream):
+            return like.new_empty(shape, dtype=dtype)
+    return new
+
+
 def make_desc(hidden: int, ffn: int, n_experts: int, top_k: int, n_shared: int = 0,
               dtype: str = "bf16", bias_group_tokens: int = 0,
               gate_mode: str = "renormalized", weight_layout: str = "row_major") -> LayerDesc:
@@ -243,7 +255,7 @@ def prism_balance_loss(desc: LayerDesc, logits, topk_idx, workspace, token_mask=
               _typed(token_mask, torch.uint8, (T,), dev, "token_mask"))
     o = outputs
     if o is None:
-        new = logits.new_empty
+        new = _new_on(stream, logits)
         o = BalanceOut(new((G,)), new((G, E), dtype=i32), new((G, E)), new((G,), dtype=i32))
         made = o.loss.data_ptr(), o.counts.data_ptr(), o.probs.data_ptr(), o.n_tokens.data_ptr()
     else:
@@ -269,7 +281,7 @@ def prism_route_backward(desc: LayerDesc, logits, topk_idx, balance: Optional[Ba
     dev = torch.cuda.current_device()
     logits_ptr = _typed(logits, f32, (T, E), dev, "logits")
     if d_logits is None:
-        d_logits = torch.empty_like(logits)
+        d_logits = _new_on(stream, logits)((T, E))
         d_ptr = d_logits.data_ptr()
     else:
         d_ptr = _typed(d_logits, f32, (T, E), dev, "d_logits")
@@ -554,9 +566,9 @@ def _float_dtype(t: torch.Tensor, what: str) -> int:
     return _FLOAT_DTYPES[t.dtype]
 
 
-def _out_i8(out: Optional[I8Matrix], rows: int, cols: int, like: torch.Tensor) -> I8Matrix:
+def _out_i8(out: Optional[I8Matrix], rows: int, cols: int, like: torch.Tensor, stream) -> I8Matrix:
     if out is None:
-        return I8Matrix(like.new_empty((_i8_bytes(rows, cols),), dtype=torch.uint8), rows, cols)
+        return I8Matrix(_new_on(stream, like)((_i8_bytes(rows, cols),), dtype=torch.uint8), rows, cols)
     if (out.rows, out.cols) != (rows, cols):
         raise PrismError(f"out is an 8-bit matrix of {out.rows} x {out.cols}, not {rows} x {cols}")
     return out
@@ -568,7 +580,7 @@ def prism_quantize_i8(src, out: Optional[I8Matrix] = None, stream=None) -> I8Mat
     dtype = _float_dtype(src, "src")
     ptr, ld = _rows_ptr(src, dev, "src")
     rows, cols = src.shape
-    o = _out_i8(out, rows, cols, src)
+    o = _out_i8(out, rows, cols, src, stream)
     _check(load_library().prism_quantize_i8(ptr, dtype, ld, rows, cols, _bytes_on(o.data, dev, "out"), _stream_on(dev, stream)),
            "prism_quantize_i8")
     return o
@@ -581,7 +593,7 @@ def prism_pack_i8(q, scale, out: Optional[I8Matrix] = None, stream=None) -> I8Ma
         raise PrismError(f"q has to be int8, not {q.dtype}")
     ptr, ld = _rows_ptr(q, dev, "q")
     rows, cols = q.shape
-    o = _out_i8(out, rows, cols, q)
+    o = _out_i8(out, rows, cols, q, stream)
     _check(load_library().prism_pack_i8(ptr, ld, _typed(scale, torch.float32, (rows,), dev, "scale"), rows, cols,
                                         _bytes_on(o.data, dev, "out"), _stream_on(dev, stream)), "prism_pack_i8")
     return o
@@ -599,7 +611,7 @@ def prism_matmul_i8(a: I8Matrix, b: I8Matrix, workspace, out=None, dtype=torch.b
         raise PrismError(f"rows of {a.cols} and of {b.cols} elements")
     dev = torch.cuda.current_device()
     if out is None:
-        out = b.data.new_empty((a.rows, b.rows), dtype=dtype)
+        out = _new_on(stream, b.data)((a.rows, b.rows), dtype=dtype)
         ptr, ldo = out.data_ptr(), b.rows
     else:
         if out.shape != (a.rows, b.rows):

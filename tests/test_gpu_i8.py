@@ -445,6 +445,36 @@ def test_router_and_experts_of_a_training_step():
     assert torch.isfinite(out).all()
 
 
+@pytest.mark.parametrize("call", ["quantize", "pack", "matmul", "balance", "backward"])
+def test_outputs_of_another_stream_do_not_take_memory_that_this_one_still_reads(call):
+    desc = P.make_desc(64, 64, 256, 8)
+    v = _rows(512, 512, F32, 1)
+    q, scale = P.prism_quantize_i8(v).values()
+    a, b, ws = P.prism_quantize_i8(v), P.prism_quantize_i8(v), P.alloc_matmul_i8_workspace(512, 512, 512)
+    logits = _rows(1024, 256, F32, 2)
+    idx, wsb = logits.topk(8, 1).indices.int(), P.alloc_balance_workspace(desc)
+    d_gate = _rows(1024, 8, F32, 3)
+    run, nbytes = {"quantize": (lambda s: P.prism_quantize_i8(v, stream=s).data, a.data.numel()),
+                   "pack": (lambda s: P.prism_pack_i8(q, scale, stream=s).data, a.data.numel()),
+                   "matmul": (lambda s: P.prism_matmul_i8(a, b, ws, dtype=F32, stream=s), 512 * 512 * 4),
+                   "balance": (lambda s: P.prism_balance_loss(desc, logits, idx, wsb, group_tokens=1, stream=s).probs, 1024 * 256 * 4),
+                   "backward": (lambda s: P.prism_route_backward(desc, logits, idx, d_gate=d_gate, stream=s), 1024 * 256 * 4)}[call]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    want = run(None).clone()
+    old = [torch.full((nbytes,), 77, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    kept = [torch.empty_like(o) for o in old]
+    torch.cuda.synchronize()
+    torch.cuda._sleep(20_000_000)
+    for k, o in zip(kept, old):
+        k.copy_(o)
+    del old, o                       # freed here, read later by this stream
+    got = run(side)
+    torch.cuda.synchronize()
+    assert all(bool((k == 77).all()) for k in kept)
+    assert torch.equal(got, want)
+
+
 def test_binding_refuses_what_does_not_fit():
     a, b = P.prism_quantize_i8(_rows(4, 64, BF16, 1)), P.prism_quantize_i8(_rows(5, 65, BF16, 1))
     ws = P.alloc_matmul_i8_workspace(4, 5, 65)
