@@ -32,14 +32,15 @@ struct RowArgs {
   int T, E, k;
   int group;                  // tokens of a group
   int parts, part_rows;       // workgroups of a group and the tokens of each
+  int first_wg;               // workgroups of the launches before this one
 };
 
-// Tokens [first, end) of this workgroup: part blockIdx.x % parts of group blockIdx.x / parts.
+// Tokens [first, end) of this workgroup: of the workgroups of all launches, part w % parts of group w / parts.
 struct Rows {
   int group, part, first, end;
 };
 __device__ __forceinline__ Rows rows_of(const RowArgs& a) {
-  const int g = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
+  const int w = a.first_wg + blockIdx.x, g = w / a.parts, part = w % a.parts;
   const long long begin = (long long)g * a.group;     // (groups may be longer than the batch)
   const int stop = (int)min(begin + a.group, (long long)a.T);
   const int first = (int)min(begin + (long long)part * a.part_rows, (long long)stop);
@@ -440,7 +441,9 @@ template <typename Fn> void with_lanes(int E, Fn&& fn) {
 }
 
 constexpr int kBackParts = 2048;  // of route_backward_kernel, about: it leaves no sums to be added
-constexpr int kMaxGroups = PRISM_MAX_BALANCE_GROUPS;   // (a workgroup each: below 2^32 threads)
+constexpr int kMaxGroups = PRISM_MAX_BALANCE_GROUPS;
+constexpr int kMaxGrid = 1 << 21; // workgroups of a launch of balance_kernel: a grid has fewer than 2^32 threads
+static_assert((long long)kMaxGrid * kThreads < 1LL << 32 && (long long)kMaxGroups * kBackThreads < 1LL << 32, "threads of a grid");
 
 // The groups of a batch, and how many workgroups share one: at least one pass of rows each, and one workgroup for up to
 // `few` passes (another pass takes less than the launch that adds the parts).
@@ -463,7 +466,7 @@ prism_status launch_balance(const prism_layer_desc& d, const float* logits, cons
                             int group_tokens, int T, float* loss, int32_t* counts, float* probs, int32_t* n_tokens,
                             void* workspace, hipStream_t st) {
   if (T == 0 && group_tokens > 0) return PRISM_OK;    // no groups
-  RowArgs a{logits, topk_idx, mask, T, d.n_experts, d.top_k, 0, 1, 0};
+  RowArgs a{logits, topk_idx, mask, T, d.n_experts, d.top_k, 0, 1, 0, 0};
   prism_status status = PRISM_OK;
   with_lanes(a.E, [&](auto lanes) {
     constexpr int LPR = decltype(lanes)::value;
@@ -473,8 +476,10 @@ prism_status launch_balance(const prism_layer_desc& d, const float* logits, cons
       return;
     }
     const Partial partial = partial_of(workspace, a.E);
-    hipLaunchKernelGGL((balance_kernel<LPR>), dim3((unsigned)G * a.parts), dim3(kThreads), 0, st, a, partial, counts, probs, n_tokens,
-                       loss);
+    const int wgs = G * a.parts;            // (more than kParts of them: a group each)
+    for (a.first_wg = 0; a.first_wg < wgs; a.first_wg += kMaxGrid)
+      hipLaunchKernelGGL((balance_kernel<LPR>), dim3((unsigned)std::min(wgs - a.first_wg, kMaxGrid)), dim3(kThreads), 0, st, a, partial,
+                         counts, probs, n_tokens, loss);
     if (a.parts > 1) {
       constexpr int kLanes = std::min(LPR, kPieceLanes);
       const int pieces = ceil_div(a.E, 4 * kLanes);
@@ -491,7 +496,7 @@ prism_status launch_route_backward(const prism_layer_desc& d, const float* logit
                                    int group_tokens, int T, const int32_t* counts, const int32_t* n_tokens, const float* d_loss,
                                    const float* d_gate, float* d_logits, hipStream_t st) {
   if (T == 0) return PRISM_OK;
-  BackwardArgs b{{logits, topk_idx, mask, T, d.n_experts, d.top_k, 0, 1, 0}, d_gate, counts, n_tokens, d_loss, d_logits, d.gate_mode == PRISM_GATES_SOFTMAX_ALL};
+  BackwardArgs b{{logits, topk_idx, mask, T, d.n_experts, d.top_k, 0, 1, 0, 0}, d_gate, counts, n_tokens, d_loss, d_logits, d.gate_mode == PRISM_GATES_SOFTMAX_ALL};
   prism_status status = PRISM_OK;
   with_lanes(b.r.E, [&](auto lanes) {
     constexpr int LPR = decltype(lanes)::value;
