@@ -148,14 +148,17 @@ Partial partial_of(void* base, int E) {
 }
 
 // Sums over a part of a group's tokens.  parts == 1: the group's results; else partial sums for finish_kernel.  A lane adds the
-// probabilities of its experts over its rows in fp32 (16 of them where 65536 tokens of 256 experts make 256 parts), the
-// wavefronts' sums are added in their order; the counts are whole numbers, whose order does not matter.
+// probabilities of its experts over kHeldRows rows in fp32 and these sums in 64 bits, so that their error does not grow with
+// the number of tokens (1024 equal rows of a lane in one fp32 sum: off by up to 2^-16; 65536 tokens of 256 experts are 16 of a lane);
+// the wavefronts' sums are added in their order; the counts are whole numbers, whose order does not matter.
+constexpr int kHeldRows = 16;
 template <int LPR>
 __global__ __launch_bounds__(kThreads) void balance_kernel(const RowArgs a, const Partial partial, int32_t* __restrict__ counts,
                                                            float* __restrict__ probs, int32_t* __restrict__ n_tokens,
                                                            float* __restrict__ loss) {
   constexpr int kRows = 64 / LPR;           // rows a wavefront holds
   constexpr int kAhead = ahead_of<LPR>;     // ... and sets of them in flight
+  static_assert(kHeldRows % kAhead == 0, "whole sets");
   constexpr int kWaves = kThreads / 64;
   __shared__ int s_counts[kMaxE], s_n;
   __shared__ f32x4 s_sum[kWaves][LPR];
@@ -178,6 +181,8 @@ __global__ __launch_bounds__(kThreads) void balance_kernel(const RowArgs a, cons
   if (live_rows > 0) atomicAdd(&s_n, live_rows);
   const int e0 = (lane % LPR) * 4;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  double earlier[4] = {0., 0., 0., 0.};
+  int held = 0;                             // rows in sum
   for (int row0 = r.first + wave * kRows * kAhead; row0 < r.end; row0 += kWaves * kRows * kAhead) {
     f32x4 v[kAhead];
     bool live[kAhead];
@@ -193,7 +198,16 @@ __global__ __launch_bounds__(kThreads) void balance_kernel(const RowArgs a, cons
 #pragma unroll
       for (int i = 0; i < 4; ++i) sum[i] += live[u] ? v[u][i] : 0.f;
     }
+    held += kAhead;
+    if (held == kHeldRows) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) earlier[i] += (double)sum[i];
+      sum = f32x4{0.f, 0.f, 0.f, 0.f};
+      held = 0;
+    }
   }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sum[i] = (float)(earlier[i] + (double)sum[i]);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {             // the rows of the wavefront
     if constexpr (LPR <= 1) sum[i] += row_xor<1>(sum[i]);

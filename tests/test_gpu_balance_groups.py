@@ -44,3 +44,22 @@ def test_more_groups_than_one_grid_has_workgroups(T, group):
     p = torch.softmax(logits.double(), 1)
     want, size = p * (u - (u * p).sum(1, keepdim=True)), p * (u.abs() + (u.abs() * p).sum(1, keepdim=True))
     assert bool(((d.double() - want).abs() <= (2 * R.relative_error_of_p(6.0) + 12 * R.EPS) * size + 1e-38).all())
+
+
+@pytest.mark.parametrize("E,group", [(3, 1 << 20), (40, 1 << 16), (256, 1 << 14), (256, (1 << 14) - 77)])
+def test_the_error_of_a_long_group_does_not_grow_with_it(E, group):
+    """Equal rows, whose probabilities a sum of fp32 rounds the same way a thousand times; so many groups that each is one workgroup's."""
+    G, k = 129, 1
+    T = G * group
+    row = torch.randn(E, generator=torch.Generator().manual_seed(E), dtype=torch.float32).clamp(-3, 3).cuda()
+    logits = row.expand(T, E).contiguous()
+    idx = (torch.arange(T, device="cuda", dtype=torch.int32) % E)[:, None].contiguous()
+    desc = P.make_desc(64, 64, E, k)
+    b = P.prism_balance_loss(desc, logits, idx, P.alloc_balance_workspace(desc), group_tokens=group)
+    p = torch.softmax(row.double(), 0)
+    # the derived error of a p; 15 additions of a lane's rows, their sum, at most 6 lanes' and 15 wavefronts' additions, the mean
+    tol = R.relative_error_of_p(6.0) + (15 + 1 + 6 + 15 + 1) * R.EPS
+    assert bool(((b.probs.double() - p).abs() <= tol * p).all()), float(((b.probs.double() - p).abs() / p).max() / R.EPS)
+    loss = E / (k * group) * (b.counts.double() * p).sum(1)
+    assert torch.equal(b.counts.sum(1), b.n_tokens)
+    assert bool(((b.loss.double() - loss).abs() <= (tol + R.EPS) * loss).all())
