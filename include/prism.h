@@ -410,8 +410,8 @@ prism_status prism_pack_weights(const void* src, int32_t rows, int32_t cols, voi
  *   src  [rows, cols] of prism_dtype src_dtype, ld elements from row to row; aligned to its elements
  * prism_pack_i8: the same from bytes and scales that exist already (bytes are taken as they are, -128 too).
  *   src  [rows, cols], ld bytes from row to row;  scale [rows]
- * prism_matmul_i8: out[i,j] = (sum over l < k of a[i,l] b[j,l]) * scale_a[i] * scale_b[j], the sum exact, one rounding
- *   at each product and one to out_dtype.  (Contractions that the library shares among workgroups: the fp32 values of
+ * prism_matmul_i8: out[i,j] = ((sum over l < k of a[i,l] b[j,l]) * scale_a[i]) * scale_b[j] in fp32: the sum exact, one rounding of
+ *   it, one at each product and one to out_dtype.  (Contractions that the library shares among workgroups: the fp32 values of
  *   up to 8 parts are added in their order.)
  *   a  [m,k], b [n,k] 8-bit matrices;  out [m,n] of prism_dtype out_dtype, ldo elements from row to row, of which only
  *   the first n are written

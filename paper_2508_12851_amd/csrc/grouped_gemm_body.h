@@ -483,7 +483,8 @@
       asm volatile("ds_read_b32 %0, %1 offset:%2\n\ts_waitcnt lgkmcnt(0)" : "=&v"(rs[i]) : "v"(a), "n"(i * 128) : "memory");
   };
 
-  // I8: sums of whole numbers times the scales of their row and column.
+  // I8: sums of whole numbers times the scales of their row and then of their column.  (The product of the scales alone may leave
+  // fp32's range where the result does not: 1e-22 twice, or 1e20 twice and a sum of 0.)
   auto epilogue_i8 = [&](const Ctx& cx, int parity) {
     const int n_tile = GATED ? cx.nt * (BN / 2) + wn * (WN / 2) : cx.nt * BN + wn * WN;
     constexpr int NO = GATED ? NJ / 2 : NJ;
@@ -508,8 +509,8 @@
           f32x4 o;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            o[e] = (float)acc[i][j][vg * 4 + e] * (rs[i] * c0[vg][e]);
-            if constexpr (GATED) o[e] = silu(o[e]) * ((float)acc[i][j + NO][vg * 4 + e] * (rs[i] * c1[vg][e]));
+            o[e] = (float)acc[i][j][vg * 4 + e] * rs[i] * c0[vg][e];
+            if constexpr (GATED) o[e] = silu(o[e]) * ((float)acc[i][j + NO][vg * 4 + e] * rs[i] * c1[vg][e]);
           }
           if constexpr (GATED) {
             *reinterpret_cast<f32x4*>(p.Cpart + crow * p.N + n) = o;
@@ -554,7 +555,7 @@
           for (int vg = 0; vg < 4; ++vg) {
             bf16x4 b;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) b[e] = (bf16_t)((float)acc[i][j0 + jl][vg * 4 + e] * (rs[i] * c[jl][vg][e]));
+            for (int e = 0; e < 4; ++e) b[e] = (bf16_t)((float)acc[i][j0 + jl][vg * 4 + e] * rs[i] * c[jl][vg][e]);
             asm volatile("ds_write_b64 %0, %1 offset:%2" ::"v"(wr), "v"(__builtin_bit_cast(u32x2, b)), "n"(jl * 64 + vg * 16) : "memory");
           }
         u32x4 v0, v1, v2, v3;
