@@ -6,6 +6,7 @@ fallback: if the library is missing, or a call fails, an exception is raised.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from dataclasses import dataclass
@@ -125,9 +126,17 @@ def _stream_on(dev: int, stream: Optional[torch.cuda.Stream]) -> Optional[int]:
     return (torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream) or None
 
 
+_HERE = contextlib.nullcontext()
+
+
+def _memory_of(stream: Optional[torch.cuda.Stream]):
+    """Context in which the outputs of a call on `stream` are made (and filled): of that stream's memory.  What the current stream has
+    freed, it may still have to read."""
+    return _HERE if stream is None else torch.cuda.stream(stream)
+
+
 def _new_on(stream: Optional[torch.cuda.Stream], like: torch.Tensor):
-    """like.new_empty for the outputs of a call on `stream`: of that stream's memory.  What the current stream has freed, it may
-    still have to read."""
+    """like.new_empty in that context."""
     if stream is None:
         return like.new_empty
 
@@ -193,10 +202,11 @@ def prism_route(desc: LayerDesc, x, w_router, router_bias, want_logits=True, cou
                 stream=None) -> RouteOut:
     T, E, k = x.shape[0], desc.n_experts, desc.top_k
     dev = x.device
-    logits = torch.empty((T, E), dtype=torch.float32, device=dev) if want_logits else None
-    idx = torch.empty((T, k), dtype=torch.int32, device=dev)
-    gate = torch.empty((T, k), dtype=torch.float32, device=dev)
-    counts = torch.empty((E,), dtype=torch.int32, device=dev)
+    with _memory_of(stream):
+        logits = torch.empty((T, E), dtype=torch.float32, device=dev) if want_logits else None
+        idx = torch.empty((T, k), dtype=torch.int32, device=dev)
+        gate = torch.empty((T, k), dtype=torch.float32, device=dev)
+        counts = torch.empty((E,), dtype=torch.int32, device=dev)
     _check(load_library().prism_route(ctypes.byref(desc), _ptr(x), _ptr(w_router), _ptr(router_bias),
                                       T, _ptr(logits), _ptr(idx), _ptr(gate), _ptr(counts),
                                       _ptr(counts_accum), _stream(stream)), "prism_route")
@@ -311,9 +321,10 @@ def prism_dispatch(desc: LayerDesc, topk_idx, local_mask, workspace, stream=None
     T, E, k = topk_idx.shape[0], desc.n_experts, desc.top_k
     dev = topk_idx.device
     i32 = dict(dtype=torch.int32, device=dev)
-    src = torch.full((2, T * k), -1, **i32)     # one fill for both lists
-    out = DispatchOut(src[0], torch.empty((E + 1,), **i32), src[1], torch.empty((E + 1,), **i32),
-                      torch.empty((2,), **i32), torch.empty((2,), dtype=torch.int64, device=dev))
+    with _memory_of(stream):
+        src = torch.full((2, T * k), -1, **i32)     # one fill for both lists
+        out = DispatchOut(src[0], torch.empty((E + 1,), **i32), src[1], torch.empty((E + 1,), **i32),
+                          torch.empty((2,), **i32), torch.empty((2,), dtype=torch.int64, device=dev))
     _check(load_library().prism_dispatch(ctypes.byref(desc), _ptr(topk_idx), _ptr(local_mask), T,
                                          _ptr(out.local_src), _ptr(out.local_offsets),
                                          _ptr(out.remote_src), _ptr(out.remote_offsets),
@@ -333,7 +344,7 @@ def prism_expert_ffn(desc: LayerDesc, x, weights: WeightTable, local_src, local_
     T = x.shape[0]
     rows = T * desc.top_k + desc.n_shared * T
     if y is None:
-        y = torch.empty((rows, desc.hidden), dtype=torch_dtype(desc), device=x.device)
+        y = _new_on(stream, x)((rows, desc.hidden), dtype=torch_dtype(desc))
         _clear_rows(desc, local_offsets, T * desc.top_k, y, stream)
     _check(load_library().prism_expert_ffn(ctypes.byref(desc), _ptr(x), ctypes.byref(weights.struct),
                                            _ptr(local_src), _ptr(local_offsets), T, _ptr(y),
@@ -346,7 +357,7 @@ def prism_combine(desc: LayerDesc, y, local_src, local_offsets, topk_gate, works
                   stream=None) -> torch.Tensor:
     T = topk_gate.shape[0]
     if out is None:
-        out = torch.empty((T, desc.hidden), dtype=torch_dtype(desc), device=y.device)
+        out = _new_on(stream, y)((T, desc.hidden), dtype=torch_dtype(desc))
     _check(load_library().prism_combine(ctypes.byref(desc), _ptr(y), _ptr(local_src),
                                         _ptr(local_offsets), _ptr(topk_gate), T, _ptr(out),
                                         _ptr(workspace), workspace.numel(), _stream(stream)),
@@ -381,7 +392,10 @@ def prism_moe_layer(desc: LayerDesc, x, w_router, router_bias, weights: WeightTa
                     stream=None, stage_events=None) -> LayerOut:
     """stage_events: optional ctypes array of 2*len(STAGES) hipEvent_t handles (see prism.h)."""
     T = x.shape[0]
-    o = alloc_layer_out(desc, T, x.device) if outputs is None else outputs
+    o = outputs
+    if o is None:
+        with _memory_of(stream):
+            o = alloc_layer_out(desc, T, x.device)
     lib = load_library()
     if stage_events is not None:
         _check(lib.prism_moe_layer_traced(ctypes.byref(desc), _ptr(x), _ptr(w_router),
@@ -435,8 +449,9 @@ def prism_layer_permutation(desc: LayerDesc, T: int, workspace, stream=None) -> 
     """Copies of the permutation the last whole-layer call left in `workspace` (see prism.h)."""
     i32 = dict(dtype=torch.int32, device=workspace.device)
     A = T * desc.top_k
-    p = LayerPermutation(torch.full((A,), -1, **i32), torch.empty((desc.n_experts + 1,), **i32),
-                         torch.empty((A,), **i32))
+    with _memory_of(stream):
+        p = LayerPermutation(torch.full((A,), -1, **i32), torch.empty((desc.n_experts + 1,), **i32),
+                             torch.empty((A,), **i32))
     _check(load_library().prism_layer_permutation(ctypes.byref(desc), T, _ptr(workspace),
                                                   workspace.numel(), _ptr(p.local_src),
                                                   _ptr(p.local_offsets), _ptr(p.inv), _stream(stream)),
@@ -477,7 +492,7 @@ def prism_ceiling_hbm_read_pattern(src, out, n_workgroups: int, loads_in_flight:
 def prism_pack_remote(desc: LayerDesc, x, remote_src, remote_offsets, stream=None) -> torch.Tensor:
     """Activation rows to ship, in remote-list order ([T*k, H]; rows past the remote count are zero)."""
     T = x.shape[0]
-    packed = torch.empty((T * desc.top_k, desc.hidden), dtype=x.dtype, device=x.device)
+    packed = _new_on(stream, x)((T * desc.top_k, desc.hidden))
     _clear_rows(desc, remote_offsets, T * desc.top_k, packed, stream)
     _check(load_library().prism_pack_remote(ctypes.byref(desc), _ptr(x), _ptr(remote_src),
                                             _ptr(remote_offsets), T, _ptr(packed), _stream(stream)),
@@ -509,7 +524,7 @@ def prism_debug_check_weights(desc: LayerDesc, weights: WeightTable, local_mask)
 def prism_pack_weights(w, stream=None) -> torch.Tensor:
     """Row-major bf16 weight matrix -> the layout of 16 x 32 tiles (a new tensor of the same shape)."""
     rows, cols = w.shape
-    packed = torch.empty_like(w)
+    packed = _new_on(stream, w)((rows, cols))
     _check(load_library().prism_pack_weights(_ptr(w), rows, cols, _ptr(packed), _stream(stream)),
            "prism_pack_weights")
     return packed
