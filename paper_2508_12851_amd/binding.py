@@ -158,25 +158,70 @@ def torch_dtype(desc: LayerDesc) -> torch.dtype:
     return torch.float32 if desc.dtype == PRISM_F32 else torch.bfloat16
 
 
+def _sizes_of(triples: Sequence) -> List[tuple]:
+    """What is known of the gate, up and down matrices of some experts, for _check_sizes: the fewest bytes of one, the sizes of their
+    elements, the (rows, cols) of those that are 8-bit matrices.  None for an expert that is not there."""
+    out = []
+    for i in range(3):
+        ws = [t[i] for t in triples if t is not None]
+        data = [w.data if isinstance(w, I8Matrix) else w for w in ws]
+        out.append((min((d.numel() * d.element_size() for d in data), default=None), {d.element_size() for d in data},
+                    {(w.rows, w.cols) for w in ws if isinstance(w, I8Matrix)}))
+    return out
+
+
+def _check_sizes(sizes: List[tuple], desc: LayerDesc) -> None:
+    """Refuses matrices that the layer's calls would read beyond their end, or whose bytes are something else."""
+    H, F, i8 = desc.hidden, desc.ffn, desc.weight_layout == WEIGHT_LAYOUTS["int8"]
+    for (fewest, elements, shapes), (rows, cols), what in zip(sizes, ((F, H), (F, H), (H, F)), ("w_gate", "w_up", "w_down")):
+        if fewest is None:
+            continue
+        if i8 and elements != {1}:
+            raise PrismError(f"{what} has elements of {max(elements)} bytes in a layer with 8-bit weights")
+        if shapes and not (i8 and shapes == {(rows, cols)}):
+            raise PrismError(f"{what} has 8-bit matrices of {sorted(shapes)} in a layer that takes {'' if i8 else 'others, '}{rows} x {cols}")
+        need = _i8_bytes(rows, cols) if i8 else rows * cols * (4 if desc.dtype == PRISM_F32 else 2)
+        if fewest < need:
+            raise PrismError(f"{what} has {fewest} bytes, {rows} x {cols} of this layer takes {need}")
+
+
 class WeightTable:
     """Device arrays of device pointers to the expert weight matrices.
 
     experts[e] is (w_gate[F,H], w_up[F,H], w_down[H,F]) or None for an expert
-    that is not hosted here; shared is a list of S such triples.  The tensors
-    are kept alive by this object.
+    that is not hosted here; shared is a list of S such triples.  A matrix is a
+    tensor or an I8Matrix.  They are kept alive by this object, and the calls
+    refuse a table whose matrices are too small for the layer.
     """
 
     def __init__(self, experts: Sequence, shared: Sequence = (), device="cuda"):
         self.keep = (list(experts), list(shared))
 
         def table(items, i):
-            ptrs = [0 if it is None else _ptr(it[i]) for it in items]
+            ptrs = [0 if it is None else _ptr(it[i].data if isinstance(it[i], I8Matrix) else it[i]) for it in items]
             if not ptrs:
                 return None
             return torch.tensor(ptrs, dtype=torch.int64, device=device)
 
         self.tables = [table(experts, i) for i in range(3)] + [table(shared, i) for i in range(3)]
         self.struct = ExpertWeights(*[None if t is None else t.data_ptr() for t in self.tables])
+        self._sizes = _sizes_of(self.keep[0] + self.keep[1])
+        self._fits = None           # (hidden, ffn, dtype, layout) that the matrices were last found large enough for
+
+    def admit(self, e: int, triple: Sequence) -> None:
+        """Keeps the matrices of routed expert e from now on; whoever calls this writes their addresses into the tables."""
+        self.keep[0][e] = triple
+        self._sizes = self._fits = None
+
+    def struct_for(self, desc: LayerDesc):
+        """The struct as the calls of this layer take it."""
+        layer = (desc.hidden, desc.ffn, desc.dtype, desc.weight_layout)
+        if self._fits != layer:
+            if self._sizes is None:
+                self._sizes = _sizes_of(self.keep[0] + self.keep[1])
+            _check_sizes(self._sizes, desc)
+            self._fits = layer
+        return ctypes.byref(self.struct)
 
 
 def workspace_bytes(desc: LayerDesc, max_tokens: int) -> int:
@@ -346,7 +391,7 @@ def prism_expert_ffn(desc: LayerDesc, x, weights: WeightTable, local_src, local_
     if y is None:
         y = _new_on(stream, x)((rows, desc.hidden), dtype=torch_dtype(desc))
         _clear_rows(desc, local_offsets, T * desc.top_k, y, stream)
-    _check(load_library().prism_expert_ffn(ctypes.byref(desc), _ptr(x), ctypes.byref(weights.struct),
+    _check(load_library().prism_expert_ffn(ctypes.byref(desc), _ptr(x), weights.struct_for(desc),
                                            _ptr(local_src), _ptr(local_offsets), T, _ptr(y),
                                            _ptr(workspace), workspace.numel(), _stream(stream)),
            "prism_expert_ffn")
@@ -399,7 +444,7 @@ def prism_moe_layer(desc: LayerDesc, x, w_router, router_bias, weights: WeightTa
     lib = load_library()
     if stage_events is not None:
         _check(lib.prism_moe_layer_traced(ctypes.byref(desc), _ptr(x), _ptr(w_router),
-                                          _ptr(router_bias), ctypes.byref(weights.struct),
+                                          _ptr(router_bias), weights.struct_for(desc),
                                           _ptr(local_mask), T, _ptr(o.out), _ptr(o.topk_idx),
                                           _ptr(o.topk_gate), _ptr(o.counts), _ptr(counts_accum),
                                           _ptr(o.remote_src), _ptr(o.remote_offsets),
@@ -409,7 +454,7 @@ def prism_moe_layer(desc: LayerDesc, x, w_router, router_bias, weights: WeightTa
                "prism_moe_layer_traced")
         return o
     _check(load_library().prism_moe_layer(ctypes.byref(desc), _ptr(x), _ptr(w_router),
-                                          _ptr(router_bias), ctypes.byref(weights.struct),
+                                          _ptr(router_bias), weights.struct_for(desc),
                                           _ptr(local_mask), T, _ptr(o.out), _ptr(o.topk_idx),
                                           _ptr(o.topk_gate), _ptr(o.counts), _ptr(counts_accum),
                                           _ptr(o.remote_src), _ptr(o.remote_offsets),
@@ -428,7 +473,7 @@ def prism_moe_layer_static(desc: LayerDesc, x, w_router, router_bias, weights: W
     supplies every output buffer)."""
     o = outputs
     _check(load_library().prism_moe_layer_static(ctypes.byref(desc), _ptr(x), _ptr(w_router),
-                                                 _ptr(router_bias), ctypes.byref(weights.struct),
+                                                 _ptr(router_bias), weights.struct_for(desc),
                                                  _ptr(local_mask), x.shape[0], _ptr(o.out),
                                                  _ptr(o.topk_idx), _ptr(o.topk_gate), _ptr(o.counts),
                                                  _ptr(counts_accum), _ptr(o.remote_src),
@@ -514,7 +559,7 @@ def prism_combine_remote(desc: LayerDesc, y_remote, remote_src, remote_offsets, 
 def prism_debug_check_weights(desc: LayerDesc, weights: WeightTable, local_mask) -> None:
     """Blocking check that every hosted and every shared expert has usable weight pointers."""
     bad = ctypes.c_int32(-1)
-    code = load_library().prism_debug_check_weights(ctypes.byref(desc), ctypes.byref(weights.struct),
+    code = load_library().prism_debug_check_weights(ctypes.byref(desc), weights.struct_for(desc),
                                                     _ptr(local_mask), ctypes.byref(bad))
     if code != 0:
         what = f"expert {bad.value}" if bad.value >= 0 else "arguments"

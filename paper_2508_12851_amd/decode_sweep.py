@@ -36,7 +36,7 @@ class Stack:
         self.B, self.torch = B, torch
         self.L, self.T, self.H, self.F, self.E, self.k = n_layers, T, H, F, E, k
         self.desc = B.make_desc(H, F, E, k, 0, "bf16", 0, weight_layout="int8" if weights == "int8" else "row_major")
-        load = (lambda w: B.prism_quantize_i8(w).data) if weights == "int8" else (lambda w: w)
+        load = B.prism_quantize_i8 if weights == "int8" else (lambda w: w)
         gen = torch.Generator(device="cuda").manual_seed(seed)
 
         def normal(shape, std):

@@ -32,26 +32,33 @@ class Migrator:
         self._staged_mask = None
 
     def start(self, table, host_experts: Dict[int, Sequence], new_mask: np.ndarray) -> None:
-        """host_experts: expert id -> (w_gate, w_up, w_down) PINNED host tensors of the admitted
-        experts.  Enqueues their upload and the pointer-table update on the copy stream."""
+        """host_experts: expert id -> (w_gate, w_up, w_down) PINNED host tensors (or 8-bit matrices in such) of the
+        admitted experts.  Enqueues their upload and the pointer-table update on the copy stream."""
+        from .binding import I8Matrix
         torch = self.torch
-        experts = table.keep[0]
         self.bytes = 0
         ptrs = [t.cpu().clone() for t in table.tables[:3]]
         # destination buffers are allocated up front (allocation is not part of the overlap)
-        dst = {e: tuple(torch.empty(w.shape, dtype=w.dtype, device="cuda") for w in ws)
-               for e, ws in host_experts.items()}
+        def on_device(w):
+            if isinstance(w, I8Matrix):
+                return I8Matrix(on_device(w.data), w.rows, w.cols)
+            return torch.empty(w.shape, dtype=w.dtype, device="cuda")
+
+        def data(w):
+            return w.data if isinstance(w, I8Matrix) else w
+
+        dst = {e: tuple(on_device(w) for w in ws) for e, ws in host_experts.items()}
         self.copy_stream.wait_stream(torch.cuda.current_stream())
         with torch.cuda.stream(self.copy_stream):
             self.begun.record()
             for e, ws in host_experts.items():
-                for i, w in enumerate(ws):
+                for i, (w, to) in enumerate(zip(map(data, ws), map(data, dst[e]))):
                     if not w.is_pinned():
                         raise ValueError("migration sources must be pinned host tensors")
-                    dst[e][i].copy_(w, non_blocking=True)
+                    to.copy_(w, non_blocking=True)
                     self.bytes += w.numel() * w.element_size()
-                    ptrs[i][e] = dst[e][i].data_ptr()
-                experts[e] = dst[e]
+                    ptrs[i][e] = to.data_ptr()
+                table.admit(e, dst[e])
             # entries of the admitted experts only change here; running layers never read them
             self._ptr_host = [p.pin_memory() for p in ptrs]
             for i in range(3):
