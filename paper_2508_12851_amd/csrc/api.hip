@@ -53,6 +53,17 @@ static prism_status check_weights(const prism_layer_desc& d, const prism_expert_
   return PRISM_OK;
 }
 
+// 8-bit experts: buffer addressing uses 32-bit byte offsets, so every operand must stay below 4 GiB.
+static prism_status check_i8_operands(const prism_layer_desc& d, int T) {
+  if (d.weight_layout != PRISM_WEIGHTS_INT8) return PRISM_OK;
+  constexpr size_t kMaxOperandBytes = 0xFFFF0000ull;
+  const int rows = T * (d.top_k + d.n_shared);
+  PRISM_RETURN_IF(i8_elements(rows, d.hidden) >= kMaxOperandBytes || i8_elements(rows, d.ffn) >= kMaxOperandBytes ||
+                      i8_elements(d.ffn, d.hidden) >= kMaxOperandBytes || i8_elements(d.hidden, d.ffn) >= kMaxOperandBytes,
+                  PRISM_ERR_UNSUPPORTED);
+  return PRISM_OK;
+}
+
 // The expert FFN on the buffers of a workspace, by the kind of its weights.
 static prism_status run_expert_ffn(const prism_layer_desc& d, const void* x, const prism_expert_weights& w,
                                    const int32_t* local_src, const int32_t* local_offsets, int T, void* y, const Workspace& ws,
@@ -196,6 +207,7 @@ prism_status prism_expert_ffn(const prism_layer_desc* desc, const void* x,
   PRISM_TRY(check_weights(*desc, weights));
   PRISM_RETURN_IF(local_offsets == nullptr, PRISM_ERR_INVALID_ARG);
   if (T > 0) PRISM_RETURN_IF(x == nullptr || local_src == nullptr || y == nullptr, PRISM_ERR_INVALID_ARG);
+  PRISM_TRY(check_i8_operands(*desc, T));
   Workspace ws;
   PRISM_TRY(check_workspace(*desc, T, workspace, workspace_bytes, &ws));
   return run_expert_ffn(*desc, x, *weights, local_src, local_offsets, T, y, ws, (hipStream_t)stream, nullptr, nullptr, false);
@@ -367,6 +379,7 @@ prism_status prism_moe_layer_traced(const prism_layer_desc* desc, const void* x,
     PRISM_RETURN_IF(x == nullptr || w_router == nullptr || out == nullptr || topk_idx == nullptr ||
                         topk_gate == nullptr || remote_src == nullptr,
                     PRISM_ERR_INVALID_ARG);
+  PRISM_TRY(check_i8_operands(*desc, T));
   Workspace ws;
   PRISM_TRY(check_workspace(*desc, T, workspace, workspace_bytes, &ws));
   const hipStream_t st = (hipStream_t)stream;

@@ -132,12 +132,6 @@ prism_status launch_expert_ffn_i8(const prism_layer_desc& d, const void* x, cons
                                   bool schedules_built) {
   if (deferred_splits != nullptr) *deferred_splits = nullptr;
   if (T == 0) return PRISM_OK;
-  // Buffer addressing uses 32-bit byte offsets, so every operand matrix must stay below 4 GiB.
-  constexpr size_t kMaxOperandBytes = 0xFFFF0000ull;
-  const int rows = T * (d.top_k + d.n_shared);
-  if (i8_elements(rows, d.hidden) >= kMaxOperandBytes || i8_elements(rows, d.ffn) >= kMaxOperandBytes ||
-      i8_elements(d.ffn, d.hidden) >= kMaxOperandBytes || i8_elements(d.hidden, d.ffn) >= kMaxOperandBytes)
-    return PRISM_ERR_UNSUPPORTED;
   return select_path(d, T, [&](auto path) {
     using P = decltype(path);
     return run_i8_ffn<typename P::C1, typename P::C2, P::kSplitDown, P::kStreamB, P::kRotate, P::kWidths>(

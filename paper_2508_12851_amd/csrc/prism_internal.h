@@ -236,7 +236,7 @@ prism_status launch_expert_ffn_f32(const prism_layer_desc& d, const void* x, con
                                    const int32_t* local_src, const int32_t* local_offsets, int T, void* y,
                                    void* h, hipStream_t st, void* const* stage_events);
 
-// The 8-bit layers' part of launch_expert_ffn (T > 0).
+// The 8-bit layers' part of launch_expert_ffn (T > 0); every operand is below 4 GiB (api.hip, check_i8_operands).
 prism_status launch_expert_ffn_i8(const prism_layer_desc& d, const void* x, const prism_expert_weights& w,
                                   const int32_t* local_src, const int32_t* local_offsets, int T, void* y, const Workspace& ws,
                                   hipStream_t st, void* const* stage_events, const int32_t** deferred_splits,
