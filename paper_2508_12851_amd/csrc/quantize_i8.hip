@@ -238,15 +238,19 @@ __global__ __launch_bounds__(kThreads) void pack_i8_kernel(const int8_t* __restr
 
 namespace {
 // Calls launch(lanes, held) with the lanes of a row: a wavefront where rows are many and it holds them; else as many as make one or two
-// passes of it.  Bytes in and out, TB/s (a large copy reaches 4.8): 28000 x 1408 fp32 by 64 lanes 5.7, by 256 4.9; 600 x
-// 2048 bf16 4.4 against 3.6 us; 7200 x 4096 bf16 by 256 lanes 5.7, by 512 4.4; 4096 x 14336 bf16 by 512 lanes 5.7, by 1024 4.4, by
-// 256 5.2; 7200 x 14336 fp32 4.8 by any.
+// passes of it, and of long rows half as many once there are more than CUs.  Rows from HBM (every launch another copy, 1.5 GB of
+// them), bytes in and out in TB/s (a large copy reaches 4.8): 28000 x 1408 fp32 by 64 lanes 4.8, by 256 3.9; 5001 x 2048 bf16 2.2 by
+// either; 7000 x 4096 fp32 by 256 lanes 4.9, by 512 4.3, by 64 3.6; 7200 x 4096 bf16 3.3, 2.4, 2.5; 7200 x 14336 fp32 by 512 lanes 5.25, by
+// 1024 4.5, by 256 5.1; 4096 x 14336 bf16 3.6, 2.6, 2.95.  Few rows, us: 600 x 2048 bf16 by 256 lanes 4.6, by 64 6.9; 32 x 14336 bf16 by 1024
+// lanes 5.8, by 512 7.0; 128 x 4160 4.4 against 5.3, 128 x 14336 6.1 / 7.2, but 300 x 4160 6.8 / 5.8, 300 x 14336 10.6 / 9.7, 512 x 8192 8.8 / 7.6
+// (fp32 rows alike).
+constexpr int kManyLongRows = 256;
 template <typename Fn> void with_row_lanes(const QuantizeArgs& a, Fn&& launch) {
   using std::integral_constant;
   if (a.cols <= 2048 && a.rows > 4096) launch(integral_constant<int, 64>{}, integral_constant<int, 4>{});
   else if (a.cols <= 2048) launch(integral_constant<int, 256>{}, integral_constant<int, 1>{});
   else if (a.cols <= 4096) launch(integral_constant<int, 256>{}, integral_constant<int, 2>{});
-  else if (a.rows > 512) launch(integral_constant<int, 512>{}, integral_constant<int, 4>{});
+  else if (a.rows > kManyLongRows) launch(integral_constant<int, 512>{}, integral_constant<int, 4>{});
   else launch(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
 }
 unsigned workgroups(const QuantizeArgs& a, int lanes) { return (unsigned)std::min(ceil_div(a.rows, lanes == 64 ? 4 : 1), kMaxGrid); }

@@ -36,7 +36,7 @@ def test_products_of_every_tile_and_split(m, n, k, tile, splits, dtype):
 # by the lanes that take a row: 64 (many short rows), 256, 512 (many long rows), 1024 (few); rows that are read twice beyond 16384
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("rows,cols", [(4097, 1408), (5001, 2047), (4100, 7), (4096, 2048), (33, 2049), (513, 4097), (700, 14335), (520, 16384),
-                                       (515, 16393), (512, 4100), (512, 16385), (9, 130944)])
+                                       (515, 16393), (257, 4100), (257, 16385), (256, 4100), (256, 16385), (9, 130944)])
 def test_quantisation_by_every_number_of_lanes(rows, cols, dtype):
     v = _rows(rows, cols, dtype, rows + cols)
     v[rows // 2] = 0
