@@ -144,8 +144,8 @@ const char* prism_status_string(prism_status s);
 
 /*
  * Workspace size in bytes (written to the host variable *bytes) that any
- * entry point below needs for a batch of up to max_tokens tokens of this
- * layer.  The size never shrinks as max_tokens grows, so a workspace sized for
+ * entry point below (but those with a size function of their own) needs for a
+ * batch of up to max_tokens tokens of this layer.  The size never shrinks as max_tokens grows, so a workspace sized for
  * the largest batch serves every smaller one.  The workspace must be 256-byte
  * aligned; its contents between calls are irrelevant; two calls that use the
  * same workspace must not overlap in time (run them on one stream, or give

@@ -122,8 +122,9 @@ typedef const __attribute__((address_space(4))) int4* const_int4_ptr;
 typedef const __attribute__((address_space(4))) int32_t* const_int_ptr;
 typedef const void* const __attribute__((address_space(4)))* const_ptr_table;
 
-// silu(z) = z / (1 + e^-z) with the hardware exp2 and reciprocal (each within 1 ulp;
-// the result is rounded to bf16 right after).
+// silu(z) = z / (1 + e^-z) with the hardware exp2 and reciprocal (each within 1 ulp; the result is
+// rounded to bf16 right after, or, in 8-bit layers, taken to 8 bits: their h is off by up to
+// (3 + |z|) 2^-23 of its value, which turns an integer whose quotient lies that near to a half).
 __device__ __forceinline__ float silu(float z) {
   return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896341f * z));
 }
